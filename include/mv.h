@@ -588,6 +588,209 @@ mv_status mv_sdcc_kl_bwd(const mv_kl_shape* shape, const void* hidden_teacher,
 float mv_sdcc_lambda(int32_t step, int32_t total_steps, float lambda_max, float warmup_frac);
 
 /* ---------------------------------------------------------------------------
+ * Rotary positions with several axes.
+ *
+ * mv_rope rotates the slots of a packing by their one position id.  Rows with
+ * positions of their own (drafted tokens, of which siblings share one; image
+ * and video tokens with a time, a height and a width) are rotated here: pair
+ * (i, i + rotary_dim/2), i < rotary_dim/2, turns by
+ *     pos[axis[i]][t] * theta^(-2i / rotary_dim),
+ * elements past rotary_dim pass through.  Angles in double precision (reduced
+ * to [-pi, pi] there), their cosine and sine and the rotation in fp32, one
+ * rounding to bf16.  Positions are any int32, negative ones too.
+ * ------------------------------------------------------------------------ */
+#define MV_ROPE_MAX_PAIRS 128
+#define MV_ROPE_MAX_AXES 8
+typedef struct {
+  int32_t rotary_dim;            /* even, 2 .. head_dim                             */
+  int32_t n_axes;                /* 1 .. MV_ROPE_MAX_AXES                           */
+  float theta;                   /* > 0                                             */
+  uint8_t axis[MV_ROPE_MAX_PAIRS]; /* position axis of pair i, < n_axes             */
+} mv_rope_axes_spec;
+
+/* x [n_tokens, n_heads, head_dim] bf16 with x_stride elements from one token
+ * to the next (a slice of a fused projection; >= n_heads * head_dim), pos
+ * int32 [n_axes, n_tokens]; out likewise with out_stride.  direction +1
+ * rotates, -1 applies the inverse, which is the adjoint and so the backward.
+ * out may be x itself (equal strides); any other overlap is not allowed.
+ * head_dim a multiple of 8, <= 256; strides multiples of 8. */
+mv_status mv_rope_axes(const mv_rope_axes_spec* spec, int32_t n_tokens, int32_t n_heads,
+                       int32_t head_dim, const void* x, int64_t x_stride, const int32_t* pos,
+                       int32_t direction, void* out, int64_t out_stride, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * The cache of a live view.
+ *
+ * The live view of a row (Eq. "live-view") as the thing it was decoded from:
+ * a cache whose rows are the live keys in order.  An edit (J_k, E_k) compacts
+ * it, the branches of a record (Section 4.1, with their trunk cached) and the
+ * samples of one prompt's group fork it, a finished one is freed, and rows
+ * attend over it (mv_tree_attn).  Keys are kept as they were written (already
+ * position-encoded), so a row's attention over the compacted cache is its
+ * attention under the mask of mv_attn_fwd.
+ *
+ * Layouts (caller-owned device memory):
+ *   k, v        bf16 [n_layers, n_pages, n_heads_kv, page_size, head_dim]
+ *   page_table  int32 [n_seqs, max_pages]; row r of sequence s is place
+ *               r % page_size of page page_table[s, r / page_size]; entries
+ *               past a sequence's pages are -1
+ *   seq_len     int32 [n_seqs]
+ *   page_refs   int32 [n_pages]: sequences that hold the page; 0: free
+ *   ctl         int32 [4]: the lowest page that may be free, refused entries
+ *               for lack of pages, refused malformed entries, one word unused
+ * The state lives on the device: every call is asynchronous, reads nothing
+ * back, allocates nothing and may be captured into a graph.  It takes
+ * lists of entries; entries are independent of each other and all read the
+ * state as it was before the call.  New pages are the lowest-numbered free
+ * ones, dealt in entry order, and a page that a call gives back is free from
+ * the next call on.  A malformed entry (a sequence id outside [0, n_seqs),
+ * unless -1 is said to be allowed; a repeated one where it matters) and one
+ * that finds too few pages changes nothing and is counted
+ * (mv_cache_status); pages are dealt until they do not suffice for an entry,
+ * and later entries that need some are refused too.  Calls on one cache must
+ * be ordered (one stream, or events).  Tables with entries or lengths out of
+ * range give unspecified results but no access outside the arrays.
+ * Limits: page_size 16, 32, 64, 128 or 256; head_dim 64 or 128; n_seqs and
+ * the entries of a call at most MV_CACHE_MAX_SEQS; n_pages * page_size < 2^31.
+ * ------------------------------------------------------------------------ */
+#define MV_CACHE_MAX_SEQS 8192
+typedef struct {
+  int32_t n_layers, n_pages, page_size;
+  int32_t n_heads_kv, head_dim;
+  int32_t n_seqs, max_pages;
+} mv_cache_shape;
+
+typedef struct {
+  void* k;
+  void* v;
+  int32_t* page_table;
+  int32_t* seq_len;
+  int32_t* page_refs;
+  int32_t* ctl;
+} mv_cache;
+
+typedef struct {
+  int32_t free_pages;
+  int32_t refused_pages;         /* entries refused for lack of pages since the last call   */
+  int32_t refused_entries;       /* malformed entries since the last call                   */
+} mv_cache_counts;
+
+/* Every sequence empty, every page free, the counters zero.  The pools are
+ * not touched. */
+mv_status mv_cache_reset(const mv_cache_shape* shape, const mv_cache* cache, hipStream_t stream);
+
+/* Free pages, and the refusals since the last mv_cache_status or
+ * mv_cache_reset (they are cleared).  Waits for the stream's work; not for
+ * use under stream capture. */
+mv_status mv_cache_status(const mv_cache_shape* shape, const mv_cache* cache,
+                          mv_cache_counts* host_out, hipStream_t stream);
+
+/*
+ * Room for new rows: entry b makes sequence seq_ids[b] longer by new_ptr[b+1]
+ * - new_ptr[b] rows (new_ptr int32 [n + 1], non-decreasing, inside [0, n_new]).
+ * slot (int32 [n_new]) receives, per new row, page * page_size + place, and
+ * pos (int32 [n_new], nullable) its index in the sequence; rows of a refused
+ * entry, and rows that no entry covers, get -1.  seq_ids -1 is a padded entry.  A sequence named twice is
+ * refused the second time.  An entry whose rows do not fit max_pages counts
+ * as one that lacks pages.
+ */
+mv_status mv_cache_reserve(const mv_cache_shape* shape, const mv_cache* cache, int32_t n,
+                           const int32_t* seq_ids, const int32_t* new_ptr, int32_t n_new,
+                           int32_t* slot, int32_t* pos, hipStream_t stream);
+
+/*
+ * Write the rows of one layer: K (rotated by `rope` and `pos` on the way if
+ * rope is not null; pos int32 [n_axes, n_rows]) and V of n_rows tokens to
+ * their slots.  k, v bf16 [n_rows, n_heads_kv, head_dim] with k_stride and
+ * v_stride elements from one token to the next (multiples of 8).  A slot outside the pool
+ * (-1 among them) is skipped; slots must differ.
+ */
+mv_status mv_cache_write(const mv_cache_shape* shape, const mv_cache* cache, int32_t layer,
+                         int32_t n_rows, const int32_t* slot, const void* k, int64_t k_stride,
+                         const void* v, int64_t v_stride, const mv_rope_axes_spec* rope,
+                         const int32_t* pos, hipStream_t stream);
+
+/* Workspace of mv_cache_fork and mv_cache_compact with n entries. */
+size_t mv_cache_compact_workspace_bytes(const mv_cache_shape* shape, int32_t n);
+
+/*
+ * Make sequence dst[e] a copy of src[e].  share != 0: the full pages are held
+ * by both and only the rows of a last, part-filled page are copied (a
+ * part-filled page has one holder, so appending to either never
+ * disturbs the other); share == 0: every row is copied into pages of its own.
+ * dst[e] must be empty, and no dst may be named twice.
+ */
+mv_status mv_cache_fork(const mv_cache_shape* shape, const mv_cache* cache, int32_t n,
+                        const int32_t* src, const int32_t* dst, int32_t share, void* workspace,
+                        size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Evict the spans of entry e (spans [span_ptr[e], span_ptr[e+1]) of `spans`,
+ * mv_span [n_spans], device memory: sorted, disjoint, half-open rows of
+ * src[e], clipped to its length) and close the gaps: dst[e] holds the other
+ * rows of src[e] in order.  Pages before the one with the first evicted row
+ * stay (dst == src) or become shared; the kept rows from there on are copied
+ * to new pages, and with dst == src the old ones are given back (rows cut off
+ * at the end alone are just dropped, unless a part-filled last page is shared).
+ * dst[e] must be src[e] or empty; no dst twice; a sequence compacted in place
+ * is no other entry's source.
+ */
+mv_status mv_cache_compact(const mv_cache_shape* shape, const mv_cache* cache, int32_t n,
+                           const int32_t* src, const int32_t* dst, const int32_t* span_ptr,
+                           const mv_span* spans, int32_t n_spans, void* workspace,
+                           size_t workspace_bytes, hipStream_t stream);
+
+/* Empty the sequences and give their pages back.  An id named twice counts
+ * once; -1 is a padded entry. */
+mv_status mv_cache_free(const mv_cache_shape* shape, const mv_cache* cache, int32_t n,
+                        const int32_t* seq_ids, hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Attention over the cache: single tokens, trees of drafted tokens, chunks.
+ *
+ * Entry b holds the newest n = row_ptr[b+1] - row_ptr[b] rows of sequence
+ * seq_ids[b], already written; with c = seq_len - n, its row i is at cache
+ * row c + i.  Row i sees every row before c and, of the new ones, itself and
+ * those before it (tree == null), or those whose bit is set in its words of
+ * `tree`: bit a % 32 of word a / 32 stands for new row a of the same entry.
+ *     o = softmax(scale * q.k) v,   lse = log sum exp(scale * q.k)
+ * over the rows seen; a row that sees none (seq_ids -1 or out of range, a
+ * sequence shorter than n) gets o = 0, lse = -inf.  What a row does not see
+ * has no influence on it, infinities and NaN included.
+ * q, o bf16 [n_rows, n_heads_q, head_dim]; lse fp32 [n_heads_q, n_rows];
+ * row_ptr int32 [n_batch + 1], row_ptr[0] = 0, non-decreasing, at most n_rows;
+ * rows from row_ptr[n_batch] on are left as they were.
+ * A sequence may occur in several entries.  Deterministic.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+  int32_t n_batch, n_rows, n_heads_q;
+  int32_t tree_words;            /* words per row of `tree` (0: none)               */
+  int32_t max_len;               /* the longest sequence expected (0: unknown): sizes the
+                                    launch and its workspace; longer ones are right too */
+  float softmax_scale;           /* <= 0 selects 1/sqrt(head_dim)                   */
+} mv_tree_attn_shape;
+
+size_t mv_tree_attn_workspace_bytes(const mv_cache_shape* cache_shape,
+                                    const mv_tree_attn_shape* shape);
+
+mv_status mv_tree_attn(const mv_cache_shape* cache_shape, const mv_cache* cache, int32_t layer,
+                       const mv_tree_attn_shape* shape, const int32_t* seq_ids,
+                       const int32_t* row_ptr, const uint32_t* tree, const void* q, void* o,
+                       float* lse, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * The words of a tree of drafted tokens, from each row's parent (its index
+ * within the same entry, smaller than the row's own; anything else makes the
+ * row a root): bits of the row itself and of its ancestors.  tree uint32
+ * [n_rows, words]; rows and ancestors past 32 * words have no bit.  depth
+ * (int32 [n_rows], nullable) receives the number of ancestors.  Rows from
+ * row_ptr[n_batch] on are left as they were.
+ */
+mv_status mv_tree_mask(int32_t n_batch, int32_t n_rows, const int32_t* row_ptr,
+                       const int32_t* parent, int32_t words, uint32_t* tree, int32_t* depth,
+                       hipStream_t stream);
+
+/* ---------------------------------------------------------------------------
  * Kernel timing (measurement support, not part of the method).
  *
  * While enabled, every kernel the library enqueues is bracketed by a pair of
@@ -597,7 +800,8 @@ float mv_sdcc_lambda(int32_t step, int32_t total_steps, float lambda_max, float 
  * (one of "attn_fwd", "attn_bwd_dkdv", "attn_bwd_reduce",
  * "attn_bwd_dq", "lm_logits", "lm_combine", "lm_grad", "lm_dh", "lm_dw", "kl_logits",
  * "kl_combine", "kl_grad", "kl_dh", "grpo", "pack", "unpack", "rope", "materialize",
- * "ppo_clip").  Not for use
+ * "ppo_clip", "rope_axes", "cache_reserve", "cache_write", "cache_plan", "cache_move",
+ * "cache_free", "tree_mask", "tree_attn", "tree_combine").  Not for use
  * under stream capture.
  * ------------------------------------------------------------------------ */
 mv_status mv_profile_enable(int32_t on);

@@ -96,10 +96,43 @@ class GrpoShape(ctypes.Structure):
                 ("adv_eps", ctypes.c_float)]
 
 
+class RopeAxesC(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("n_axes", ctypes.c_int32),
+                ("theta", ctypes.c_float), ("axis", ctypes.c_uint8 * 128)]
+
+
+class CacheShape(ctypes.Structure):
+    _fields_ = [("n_layers", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("n_heads_kv", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("n_seqs", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32)]
+
+
+class CacheC(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+                ("seq_len", ctypes.c_void_p), ("page_refs", ctypes.c_void_p),
+                ("ctl", ctypes.c_void_p)]
+
+
+class CacheCounts(ctypes.Structure):
+    _fields_ = [("free_pages", ctypes.c_int32), ("refused_pages", ctypes.c_int32),
+                ("refused_entries", ctypes.c_int32)]
+
+    def as_dict(self):
+        return {k: getattr(self, k) for k, _ in self._fields_}
+
+
+class TreeAttnShape(ctypes.Structure):
+    _fields_ = [("n_batch", ctypes.c_int32), ("n_rows", ctypes.c_int32),
+                ("n_heads_q", ctypes.c_int32), ("tree_words", ctypes.c_int32),
+                ("max_len", ctypes.c_int32), ("softmax_scale", ctypes.c_float)]
+
+
 GRPO_STATS = ["loss", "logdiff", "clip_frac_low", "clip_frac_high", "kl_ref", "ratio_mean",
               "n_loss_tokens", "adv_abs_mean"]
 
 _vp, _sz, _i32, _f32 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32, ctypes.c_float
+_i64 = ctypes.c_int64
 _P = ctypes.POINTER
 
 
@@ -185,6 +218,27 @@ mv_sdcc_kl_bwd_workspace_bytes = _sig("mv_sdcc_kl_bwd_workspace_bytes", _sz, _P(
 mv_sdcc_kl_bwd = _sig("mv_sdcc_kl_bwd", ctypes.c_int, _P(KLShape), _vp, _vp, _vp, _vp, _vp, _vp,
                       _vp, _vp, _vp, _vp, _sz, _vp)
 mv_sdcc_lambda = _sig("mv_sdcc_lambda", _f32, _i32, _i32, _f32, _f32)
+mv_rope_axes = _sig("mv_rope_axes", ctypes.c_int, _P(RopeAxesC), _i32, _i32, _i32, _vp, _i64, _vp,
+                    _i32, _vp, _i64, _vp)
+mv_cache_reset = _sig("mv_cache_reset", ctypes.c_int, _P(CacheShape), _P(CacheC), _vp)
+mv_cache_status = _sig("mv_cache_status", ctypes.c_int, _P(CacheShape), _P(CacheC),
+                       _P(CacheCounts), _vp)
+mv_cache_reserve = _sig("mv_cache_reserve", ctypes.c_int, _P(CacheShape), _P(CacheC), _i32, _vp,
+                        _vp, _i32, _vp, _vp, _vp)
+mv_cache_write = _sig("mv_cache_write", ctypes.c_int, _P(CacheShape), _P(CacheC), _i32, _i32, _vp,
+                      _vp, _i64, _vp, _i64, _P(RopeAxesC), _vp, _vp)
+mv_cache_compact_workspace_bytes = _sig("mv_cache_compact_workspace_bytes", _sz, _P(CacheShape),
+                                        _i32)
+mv_cache_fork = _sig("mv_cache_fork", ctypes.c_int, _P(CacheShape), _P(CacheC), _i32, _vp, _vp,
+                     _i32, _vp, _sz, _vp)
+mv_cache_compact = _sig("mv_cache_compact", ctypes.c_int, _P(CacheShape), _P(CacheC), _i32, _vp,
+                        _vp, _vp, _vp, _i32, _vp, _sz, _vp)
+mv_cache_free = _sig("mv_cache_free", ctypes.c_int, _P(CacheShape), _P(CacheC), _i32, _vp, _vp)
+mv_tree_attn_workspace_bytes = _sig("mv_tree_attn_workspace_bytes", _sz, _P(CacheShape),
+                                    _P(TreeAttnShape))
+mv_tree_attn = _sig("mv_tree_attn", ctypes.c_int, _P(CacheShape), _P(CacheC), _i32,
+                    _P(TreeAttnShape), _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp)
+mv_tree_mask = _sig("mv_tree_mask", ctypes.c_int, _i32, _i32, _vp, _vp, _i32, _vp, _vp, _vp)
 
 mv_profile_enable = _sig("mv_profile_enable", ctypes.c_int, _i32)
 mv_profile_read = _sig("mv_profile_read", ctypes.c_int, ctypes.c_char_p, _P(ctypes.c_double),
@@ -205,7 +259,10 @@ EXPORTED = ["mv_status_string", "mv_last_error", "mv_version", "mv_build_view_ma
             "mv_view_mask_intervals", "mv_token_logprob_bad_targets", "mv_attn_bwd_noalloc",
             "mv_build_shared_trunk_pack", "mv_token_logprob_grpo_workspace_bytes",
             "mv_token_logprob_grpo", "mv_pack_rows_rope", "mv_unpack_rows_sum_rope",
-            "mv_build_view_mask_tiled",
+            "mv_build_view_mask_tiled", "mv_rope_axes", "mv_cache_reset", "mv_cache_status",
+            "mv_cache_reserve", "mv_cache_write", "mv_cache_compact_workspace_bytes",
+            "mv_cache_fork", "mv_cache_compact", "mv_cache_free", "mv_tree_attn_workspace_bytes",
+            "mv_tree_attn", "mv_tree_mask",
             "mv_profile_enable", "mv_profile_read"]
 
 VIEW_LIVE, VIEW_FINAL = 0, 1
@@ -710,6 +767,293 @@ def sdcc_lambda(step: int, total_steps: int, lambda_max: float = 0.1,
 
 
 # ---------------------------------------------------------------------------
+# rotary positions with several axes
+# ---------------------------------------------------------------------------
+def _need(t, dtype, what, shape=None, contiguous=True):
+    """A CUDA tensor of the current device with the given type (and shape)."""
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or not t.is_cuda:
+        raise ValueError(f"{what}: expected a {dtype} CUDA tensor")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{what} is on {t.device}, the current device is "
+                         f"cuda:{torch.cuda.current_device()}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    if contiguous and not t.is_contiguous():
+        raise ValueError(f"{what}: expected a contiguous tensor")
+
+
+def _token_stride(t, what):
+    """Elements from one token of t [n, heads, d] to the next; a token's own
+    elements lie together."""
+    n, h, d = t.shape
+    if (d > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != d):
+        raise ValueError(f"{what}: the heads of a token must lie together")
+    return t.stride(0) if n > 1 else h * d
+
+
+def _use(stream, *ts):
+    """The stream's handle; tensors made here on the current stream are kept
+    from reuse until `stream` is done with them."""
+    cur = torch.cuda.current_stream()
+    if stream is not None and stream != cur:
+        # what this call allocated may be a block whose last use is queued there
+        stream.wait_stream(cur)
+        for t in ts:
+            if t is not None:
+                t.record_stream(stream)
+    return _stream(stream)
+
+
+class RopeAxes:
+    """How the pairs of a head rotate: pair (i, i + n), n = len(axis_map), by
+    position axis ``axis_map[i]`` at frequency theta^(-i / n)."""
+
+    def __init__(self, head_dim: int, axis_map: Sequence[int], theta: float = 1e6):
+        axis = [int(a) for a in axis_map]
+        if not 1 <= len(axis) <= 128 or 2 * len(axis) > head_dim:
+            raise ValueError("axis_map: between 1 and head_dim / 2 (at most 128) pairs")
+        if min(axis) < 0:
+            raise ValueError("axis_map: axes are >= 0")
+        self.head_dim, self.rotary_dim, self.n_axes = int(head_dim), 2 * len(axis), max(axis) + 1
+        self.theta = float(theta)
+        if self.n_axes > 8:
+            raise ValueError("axis_map: at most 8 axes")
+        self.c = RopeAxesC(self.rotary_dim, self.n_axes, self.theta, (ctypes.c_uint8 * 128)(*axis))
+
+
+def _rope_pos(rope, pos, n):
+    if pos is None or pos.dim() != 2 or pos.shape[0] < rope.n_axes:
+        raise ValueError(f"pos: expected [{rope.n_axes}, {n}] position ids")
+    _need(pos, torch.int32, "pos", (pos.shape[0], n))
+
+
+def rope_axes(x, pos, rope: RopeAxes, inverse: bool = False, out=None, stream=None):
+    """x [n, H, d] bf16 (a token's heads together, tokens any multiple of 8
+    elements apart) rotated by pos int32 [n_axes, n]; ``inverse``: by the
+    negative angles, which is the backward.  ``out`` may be x."""
+    _need(x, torch.bfloat16, "x", contiguous=False)
+    if x.dim() != 3 or x.shape[2] != rope.head_dim:
+        raise ValueError(f"x: expected [n, heads, {rope.head_dim}]")
+    _rope_pos(rope, pos, x.shape[0])
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        handle = _use(stream, out)
+    else:
+        _need(out, torch.bfloat16, "out", x.shape, contiguous=False)
+        handle = _stream(stream)
+    check(mv_rope_axes(ctypes.byref(rope.c), x.shape[0], x.shape[1], x.shape[2], _ptr(x),
+                       _token_stride(x, "x"), _ptr(pos), -1 if inverse else 1, _ptr(out),
+                       _token_stride(out, "out"), handle))
+    return out
+
+
+# ---------------------------------------------------------------------------
+# the cache of a live view
+# ---------------------------------------------------------------------------
+class PagedCache:
+    """Pools of pages and the tables of the sequences that hold them, as plain
+    device tensors: k, v bf16 [n_layers, n_pages, n_heads_kv, page_size,
+    head_dim], page_table int32 [n_seqs, max_pages] (-1: none), seq_len int32
+    [n_seqs], page_refs int32 [n_pages] (holders; 0: free).  New caches are
+    empty (the pools' contents are not set)."""
+
+    def __init__(self, n_layers: int, n_pages: int, page_size: int, n_heads_kv: int,
+                 head_dim: int, n_seqs: int, max_pages: int, device="cuda", stream=None):
+        self.shape = CacheShape(n_layers, n_pages, page_size, n_heads_kv, head_dim, n_seqs,
+                                max_pages)
+        dev = torch.device(device)
+        if dev.type == "cuda" and dev.index not in (None, torch.cuda.current_device()):
+            raise ValueError(f"device {dev} is not the current one")
+        # a shape that the library refuses is refused before anything is allocated
+        if not mv_cache_compact_workspace_bytes(ctypes.byref(self.shape), 0):
+            check(mv_cache_reset(ctypes.byref(self.shape), None, None))
+        pool = (n_layers, n_pages, n_heads_kv, page_size, head_dim)
+        self.k = torch.empty(pool, dtype=torch.bfloat16, device=device)
+        self.v = torch.empty(pool, dtype=torch.bfloat16, device=device)
+        i32 = lambda *s: torch.empty(s, dtype=torch.int32, device=device)
+        self.page_table, self.seq_len = i32(n_seqs, max_pages), i32(n_seqs)
+        self.page_refs, self._ctl = i32(n_pages), i32(4)
+        self.c = CacheC(_ptr(self.k), _ptr(self.v), _ptr(self.page_table), _ptr(self.seq_len),
+                        _ptr(self.page_refs), _ptr(self._ctl))
+        self.reset(stream)
+
+    def _args(self):
+        if self.k.device.index != torch.cuda.current_device():
+            raise ValueError(f"the cache is on {self.k.device}, the current device is "
+                             f"cuda:{torch.cuda.current_device()}")
+        return ctypes.byref(self.shape), ctypes.byref(self.c)
+
+    def reset(self, stream=None) -> None:
+        """Every sequence empty, every page free."""
+        check(mv_cache_reset(*self._args(),
+                             _use(stream, self.k, self.v, self.page_table, self.seq_len,
+                                  self.page_refs, self._ctl)))
+
+    def restore(self, page_table, seq_len, page_refs) -> None:
+        """Take over a state saved from (or laid out for) a cache of this shape."""
+        for mine, theirs, what in ((self.page_table, page_table, "page_table"),
+                                   (self.seq_len, seq_len, "seq_len"),
+                                   (self.page_refs, page_refs, "page_refs")):
+            if tuple(mine.shape) != tuple(theirs.shape):
+                raise ValueError(f"{what}: expected shape {tuple(mine.shape)}")
+            mine.copy_(theirs)
+        self._ctl.zero_()
+
+    def status(self, stream=None) -> dict:
+        """free_pages, and the entries refused (for lack of pages, as malformed)
+        since the last call; waits for the stream."""
+        out = CacheCounts()
+        check(mv_cache_status(*self._args(), ctypes.byref(out), _stream(stream)))
+        return out.as_dict()
+
+
+def _need_ids(t, what, n=None):
+    _need(t, torch.int32, what)
+    if t.dim() != 1 or (n is not None and t.numel() != n):
+        raise ValueError(f"{what}: expected a vector" + (f" of {n}" if n is not None else ""))
+
+
+def cache_reserve(cache: PagedCache, seq_ids, new_ptr, n_new: int, stream=None):
+    """Room for new_ptr[b+1] - new_ptr[b] rows of sequence seq_ids[b]:
+    (slot, pos) int32 [n_new], each row's place for cache_write (-1: refused)
+    and its index in the sequence."""
+    _need_ids(seq_ids, "seq_ids")
+    _need_ids(new_ptr, "new_ptr", seq_ids.numel() + 1)
+    dev = seq_ids.device
+    slot = torch.empty(int(n_new), dtype=torch.int32, device=dev)
+    pos = torch.empty(int(n_new), dtype=torch.int32, device=dev)
+    check(mv_cache_reserve(*cache._args(), seq_ids.numel(), _ptr(seq_ids), _ptr(new_ptr),
+                           int(n_new), _ptr(slot), _ptr(pos), _use(stream, slot, pos)))
+    return slot, pos
+
+
+def cache_write(cache: PagedCache, layer: int, slot, k, v, rope: Optional[RopeAxes] = None,
+                pos=None, stream=None) -> None:
+    """K (rotated by ``rope`` and pos [n_axes, n] if given) and V, bf16 [n,
+    n_heads_kv, head_dim] (tokens any multiple of 8 elements apart), into their slots."""
+    n, s = slot.numel(), cache.shape
+    _need_ids(slot, "slot")
+    for t, what in ((k, "k"), (v, "v")):
+        _need(t, torch.bfloat16, what, (n, s.n_heads_kv, s.head_dim), contiguous=False)
+    if rope is not None:
+        if rope.head_dim != s.head_dim:
+            raise ValueError("rope is for another head_dim")
+        _rope_pos(rope, pos, n)
+    check(mv_cache_write(*cache._args(), int(layer), n, _ptr(slot), _ptr(k),
+                         _token_stride(k, "k"), _ptr(v), _token_stride(v, "v"),
+                         ctypes.byref(rope.c) if rope is not None else None,
+                         _ptr(pos) if rope is not None else None, _stream(stream)))
+
+
+def cache_workspace(cache: PagedCache, n: int) -> torch.Tensor:
+    """Workspace of cache_fork and cache_compact calls of up to n entries."""
+    nbytes = int(mv_cache_compact_workspace_bytes(ctypes.byref(cache.shape), int(n)))
+    return torch.empty(nbytes, dtype=torch.uint8, device=cache.k.device)
+
+
+def cache_fork(cache: PagedCache, src, dst, share: bool = True, workspace=None,
+               stream=None) -> None:
+    """Sequence dst[e] (empty) becomes a copy of src[e], its full pages shared
+    (or copied too)."""
+    _need_ids(src, "src")
+    _need_ids(dst, "dst", src.numel())
+    ws = workspace if workspace is not None else cache_workspace(cache, src.numel())
+    check(mv_cache_fork(*cache._args(), src.numel(), _ptr(src), _ptr(dst), 1 if share else 0,
+                        _ptr(ws), ws.numel(), _use(stream, ws if workspace is None else None)))
+
+
+def cache_compact(cache: PagedCache, src, dst, span_ptr, spans, workspace=None,
+                  stream=None) -> None:
+    """Evict rows spans[span_ptr[e] : span_ptr[e+1]] (int32 [n, 2], half-open)
+    of src[e]; dst[e] (src[e] itself, or empty) holds the others in order."""
+    _need_ids(src, "src")
+    n = src.numel()
+    _need_ids(dst, "dst", n)
+    _need_ids(span_ptr, "span_ptr", n + 1)
+    _need(spans, torch.int32, "spans")
+    if spans.dim() != 2 or spans.shape[1] != 2:
+        raise ValueError("spans: expected [n_spans, 2]")
+    ws = workspace if workspace is not None else cache_workspace(cache, n)
+    check(mv_cache_compact(*cache._args(), n, _ptr(src), _ptr(dst), _ptr(span_ptr), _ptr(spans),
+                           spans.shape[0], _ptr(ws), ws.numel(),
+                           _use(stream, ws if workspace is None else None)))
+
+
+def cache_free(cache: PagedCache, seq_ids, stream=None) -> None:
+    """Empty the sequences and give their pages back."""
+    _need_ids(seq_ids, "seq_ids")
+    check(mv_cache_free(*cache._args(), seq_ids.numel(), _ptr(seq_ids), _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# attention over the cache
+# ---------------------------------------------------------------------------
+def tree_mask(parent, row_ptr, max_rows: int, stream=None):
+    """(tree [n, words] int32 bit words, depth [n] int32) of drafted rows from
+    their parents; max_rows: the most rows of an entry."""
+    _need_ids(parent, "parent")
+    _need_ids(row_ptr, "row_ptr")
+    if row_ptr.numel() < 1:
+        raise ValueError("row_ptr: expected n_batch + 1 entries")
+    n, words = parent.numel(), max(1, (int(max_rows) + 31) // 32)
+    tree = torch.empty((n, words), dtype=torch.int32, device=parent.device)
+    depth = torch.empty(n, dtype=torch.int32, device=parent.device)
+    check(mv_tree_mask(row_ptr.numel() - 1, n, _ptr(row_ptr), _ptr(parent), words, _ptr(tree),
+                       _ptr(depth), _use(stream, tree, depth)))
+    return tree, depth
+
+
+def _tree_attn_shape(q, n_batch, tree, scale, max_len):
+    return TreeAttnShape(n_batch, q.shape[0], q.shape[1], 0 if tree is None else tree.shape[1],
+                         int(max_len), float(scale) if scale else 0.0)
+
+
+def tree_attn_workspace(cache: PagedCache, q, n_batch: int, max_len: int = 0) -> torch.Tensor:
+    s = _tree_attn_shape(q, int(n_batch), None, None, max_len)
+    nbytes = int(mv_tree_attn_workspace_bytes(ctypes.byref(cache.shape), ctypes.byref(s)))
+    return torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+
+
+def tree_attn(cache: PagedCache, layer: int, q, seq_ids, row_ptr, tree=None,
+              scale: Optional[float] = None, max_len: int = 0, workspace=None, out=None,
+              stream=None):
+    """Attention of the newest rows of each sequence (q [n, Hq, d] bf16, entry
+    b's rows row_ptr[b] .. row_ptr[b+1], already in the cache) over its rows:
+    (o [n, Hq, d] bf16, lse fp32 [Hq, n]).  ``tree`` (from tree_mask): which
+    new rows a row sees; otherwise itself and those before it.  ``max_len``:
+    the longest sequence expected, if known.  ``out``: (o, lse) to write."""
+    s = cache.shape
+    _need(q, torch.bfloat16, "q")
+    if q.dim() != 3 or q.shape[2] != s.head_dim:
+        raise ValueError(f"q: expected [n, heads, {s.head_dim}]")
+    _need_ids(seq_ids, "seq_ids")
+    B = seq_ids.numel()
+    _need_ids(row_ptr, "row_ptr", B + 1)
+    if tree is not None:
+        _need(tree, torch.int32, "tree")
+        if tree.dim() != 2 or tree.shape[0] != q.shape[0] or tree.shape[1] < 1:
+            raise ValueError("tree: expected [n, words], at least one word")
+    shape = _tree_attn_shape(q, B, tree, scale, max_len)
+    made = []
+    if out is None:
+        o = torch.empty_like(q)
+        lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
+        made += [o, lse]
+    else:
+        o, lse = out
+        _need(o, torch.bfloat16, "o", q.shape)
+        _need(lse, torch.float32, "lse", (q.shape[1], q.shape[0]))
+    if workspace is None:
+        n = int(mv_tree_attn_workspace_bytes(ctypes.byref(s), ctypes.byref(shape)))
+        workspace = torch.empty(n, dtype=torch.uint8, device=q.device)
+        made.append(workspace)
+    check(mv_tree_attn(*cache._args(), int(layer), ctypes.byref(shape), _ptr(seq_ids),
+                       _ptr(row_ptr), _ptr(tree), _ptr(q), _ptr(o), _ptr(lse), _ptr(workspace),
+                       workspace.numel(), _use(stream, *made)))
+    return o, lse
+
+
+# ---------------------------------------------------------------------------
 # kernel timing
 # ---------------------------------------------------------------------------
 KERNELS = ["attn_fwd", "attn_bwd_dkdv", "attn_bwd_reduce", "attn_bwd_dq",
@@ -717,7 +1061,8 @@ KERNELS = ["attn_fwd", "attn_bwd_dkdv", "attn_bwd_reduce", "attn_bwd_dq",
            "kl_logits", "kl_combine", "kl_wt", "kl_grad", "kl_dh",
            "grpo", "grpo_prep", "grpo_finish", "pack", "unpack", "rope", "pack_rope",
            "unpack_rope",
-           "materialize", "ppo_clip"]
+           "materialize", "ppo_clip", "rope_axes", "cache_reserve", "cache_write", "cache_plan",
+           "cache_move", "cache_free", "tree_mask", "tree_attn", "tree_combine"]
 
 
 def profile_enable(on: bool = True) -> None:

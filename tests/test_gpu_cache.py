@@ -1,0 +1,273 @@
+"""The page operators of the cache against the plain model: tables, lengths and
+holder counts equal after every call, pools bit for bit (stale rows included:
+nothing but the rows a call names is written)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache as OC
+from paper_2609_00865_amd import mv
+
+pytestmark = pytest.mark.gpu
+BF = torch.bfloat16
+
+
+def i32(x, shape=None):
+    t = torch.tensor(x, dtype=torch.int32, device="cuda")
+    return t if shape is None else t.reshape(shape)
+
+
+class Pair:
+    """The library's cache and the model, taken through the same calls."""
+
+    def __init__(self, layers=2, pages=40, page=16, heads=2, d=64, seqs=8, max_pages=12, seed=0):
+        self.gen = torch.Generator().manual_seed(seed)
+        self.c = mv.PagedCache(layers, pages, page, heads, d, seqs, max_pages)
+        self.m = OC.Cache(layers, pages, page, heads, d, seqs, max_pages)
+        fill = lambda: torch.randn(self.c.k.shape, generator=self.gen).to(BF)
+        for dev, name in ((self.c.k, "k"), (self.c.v, "v")):
+            x = fill()
+            dev.copy_(x)
+            setattr(self.m, name, x.double().numpy())
+        self.layers, self.heads, self.d = layers, heads, d
+
+    def reserve(self, ids, ptr, n_new=None):
+        n_new = ptr[-1] if n_new is None else n_new
+        slot, pos = mv.cache_reserve(self.c, i32(ids), i32(ptr), n_new)
+        a, b = self.m.reserve(ids, ptr, n_new)
+        assert slot.tolist() == a and pos.tolist() == b
+        self.same()
+        return slot
+
+    def write(self, slot):
+        n = slot.numel()
+        for layer in range(self.layers):
+            k, v = (torch.randn(n, self.heads, self.d, generator=self.gen).to(BF) for _ in range(2))
+            mv.cache_write(self.c, layer, slot, k.cuda(), v.cuda())
+            self.m.write(layer, slot.tolist(), k.double().numpy(), v.double().numpy())
+        self.same()
+
+    def add(self, ids, rows):
+        self.write(self.reserve(ids, [0] + np.cumsum(rows).tolist()))
+
+    def free(self, ids):
+        mv.cache_free(self.c, i32(ids))
+        self.m.free(ids)
+        self.same()
+
+    def fork(self, src, dst, share=True):
+        mv.cache_fork(self.c, i32(src), i32(dst), share=share)
+        self.m.fork(src, dst, share)
+        self.same()
+
+    def compact(self, src, dst, spans):
+        ptr = [0] + np.cumsum([len(x) for x in spans]).tolist()
+        flat = [list(x) for y in spans for x in y]
+        mv.cache_compact(self.c, i32(src), i32(dst), i32(ptr), i32(flat, (len(flat), 2)))
+        self.m.compact(src, dst, spans)
+        self.same()
+
+    def same(self):
+        torch.cuda.synchronize()
+        m = self.m
+        assert self.c.seq_len.tolist() == m.len
+        assert self.c.page_refs.tolist() == m.refs
+        assert np.array_equal(self.c.page_table.cpu().numpy(), m.page_table())
+        for dev, ref in ((self.c.k, m.k), (self.c.v, m.v)):
+            assert np.array_equal(dev.cpu().double().numpy(), ref)
+        for s in range(m.n_seqs):
+            assert len(m.table[s]) == -(-m.len[s] // m.page)
+
+    def status(self):
+        st = self.c.status()
+        assert st == {"free_pages": self.m.free_pages(), "refused_pages": self.m.no_pages,
+                      "refused_entries": self.m.bad}
+        self.m.no_pages = self.m.bad = 0
+
+
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
+@pytest.mark.parametrize("d", [64, 128])
+def test_reserve_write_free(page, d):
+    p = Pair(page=page, d=d, pages=24, max_pages=6, heads=3, seed=page)
+    print(f"[gpu] cache page={page} d={d}", flush=True)
+    p.add([0, 3, 5], [1, page, 2 * page + 1])
+    p.add([5, 1, 0], [page - 1, 0, page - 1])       # up to a page's end, none, across
+    p.add([0], [1])
+    p.status()
+    p.free([3, 5])
+    p.add([7, 3], [3 * page, 5])                    # the freed pages again, lowest first
+    p.free([0, 1, 3, 7])
+    assert p.m.free_pages() == 24
+    p.status()
+
+
+def test_padding_duplicates_and_bad_ids():
+    p = Pair()
+    p.add([2, -1, 4], [5, 0, 9])
+    p.reserve([2, -1, 2, 9, -3], [0, 3, 7, 9, 10, 12])        # padded rows, a repeat, bad ids
+    p.reserve([1, 3], [2, 5, 5], n_new=8)                     # rows no entry covers
+    p.reserve([1, 3, 0], [0, 4, 2, 6], n_new=5)               # falling, and past n_new
+    p.status()
+    p.free([2, 2, -1, 8, -5, 4])
+    p.status()
+    p.fork([1, 1, 1, 0], [5, 5, 1, 12])                       # a repeated, a full, a bad target
+    p.status()
+    p.compact([1, 1, 5], [1, 6, 7], [[(0, 1)], [], [(3, 2)]])  # in place and a source; not sorted
+    p.compact([1], [1], [[(2, 3), (1, 2)]])
+    p.compact([1], [1], [[(-1, 2)]])
+    p.status()
+
+
+def test_pages_run_out():
+    p = Pair(pages=7, page=16, max_pages=6)
+    p.add([0], [33])                                          # 3 pages, 4 left
+    p.reserve([1, 2, 3, 0], [0, 32, 80, 81, 95])              # 2, 3 (refused), 1 (after it), 0 new
+    p.status()
+    p.reserve([4], [0, 97])                                   # more than the table holds
+    p.status()
+    p.fork([0, 0, 0], [5, 6, 7])                              # one page each, 2 left
+    p.status()
+    p.free([1, 5, 6, 7])
+    p.compact([0], [0], [[(0, 1)]])
+    p.fork([0], [4], share=False)
+    p.fork([0], [6], share=False)
+    p.status()
+    p.free([0, 4, 6])
+    p.status()
+
+
+@pytest.mark.parametrize("share", [True, False])
+@pytest.mark.parametrize("n", [0, 1, 15, 16, 17, 48, 95])
+def test_fork(n, share):
+    p = Pair(pages=60)
+    p.add([1, 2], [n, 20])
+    p.fork([1, 2, 1, 1], [0, 3, 4, 7], share)
+    p.add([0, 1, 4], [5, 3, 17])                              # each goes on by itself
+    p.free([1])
+    p.add([7, 5], [16, 30])
+    p.free([0, 4, 7, 2, 3, 5])
+    assert p.m.free_pages() == 60
+    p.status()
+
+
+SPANS = [[], [(0, 1)], [(0, 95)], [(94, 95)], [(3, 3), (5, 9), (9, 12), (40, 64)], [(16, 32)],
+         [(33, 2 ** 31 - 1)], [(48, 1000)], [(95, 96), (200, 300)], [(1, 2), (3, 4), (5, 6), (90, 95)]]
+
+
+@pytest.mark.parametrize("spans", SPANS, ids=[str(i) for i in range(len(SPANS))])
+@pytest.mark.parametrize("where", ["in_place", "beside", "in_place_shared"])
+def test_compact(spans, where):
+    p = Pair(pages=60)
+    p.add([2, 3], [95, 20])
+    if where == "in_place_shared":
+        p.fork([2], [5])
+    p.compact([2, 3], [2, 3] if where != "beside" else [6, 0], [spans, [(0, 20)]])
+    p.add([2], [9])
+    if where != "in_place":
+        p.add([5 if where == "in_place_shared" else 6], [9])
+    p.status()
+
+
+def test_truncation_of_a_shared_page():
+    """Rows cut off inside a page that a fork still holds: the rest moves to a
+    page of its own, so that what is appended does not show in the other."""
+    p = Pair()
+    p.add([0], [48])
+    p.fork([0], [1])
+    p.compact([1], [1], [[(20, 48)]])
+    p.add([1], [10])
+    p.compact([0], [0], [[(40, 48)]])       # its last page has one holder now
+    p.add([0], [4])
+    p.status()
+
+
+def test_many_spans_and_entries():
+    p = Pair(layers=1, pages=400, heads=1, seqs=80, max_pages=20, seed=3)
+    rng = np.random.default_rng(1)
+    for lo in (0, 40):
+        p.add(list(range(lo, lo + 40)), rng.integers(0, 140, 40).tolist())
+    cut = []
+    for s in range(80):
+        at = np.sort(rng.choice(160, size=2 * int(rng.integers(0, 70)), replace=False))
+        cut.append([(int(a), int(b)) for a, b in zip(at[::2], at[1::2])])
+    order = rng.permutation(80).tolist()
+    p.compact(order, order, [cut[s] for s in order])
+    p.free(order[::2])
+    p.compact(order[1::2], order[::2], [cut[s] for s in order[1::2]])
+    p.free(list(range(80)))
+    assert p.m.free_pages() == 400
+    p.status()
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_random_calls(seed):
+    rng = np.random.default_rng(seed)
+    page = int(rng.choice([16, 32]))
+    p = Pair(layers=int(rng.integers(1, 4)), pages=int(rng.integers(9, 50)), page=page,
+             heads=int(rng.integers(1, 4)), seqs=6, max_pages=int(rng.integers(3, 9)), seed=seed)
+    print(f"[gpu] cache random seed {seed}", flush=True)
+    for _ in range(25):
+        op = rng.integers(0, 5)
+        n = int(rng.integers(1, 5))
+        ids = rng.integers(-1, 7, n).tolist()
+        if op <= 1:
+            p.add(ids, rng.integers(0, 3 * page, n).tolist())
+        elif op == 2:
+            p.free(ids)
+        elif op == 3:
+            p.fork(ids, rng.integers(-1, 7, n).tolist(), bool(rng.integers(0, 2)))
+        else:
+            cut = []
+            for s in ids:
+                at = np.sort(rng.choice(4 * page, size=2 * int(rng.integers(0, 5)), replace=False))
+                cut.append([(int(a), int(b)) for a, b in zip(at[::2], at[1::2])])
+            p.compact(ids, [s if rng.random() < .7 else int(rng.integers(0, 6)) for s in ids], cut)
+    p.status()
+
+
+def test_write_rotated_and_strided():
+    """Keys rotated on their way into the pages equal keys rotated before,
+    from slices of a fused projection; skipped slots write nothing."""
+    for d, rot in ((128, 128), (64, 40), (64, 6), (128, 66)):
+        p = Pair(d=d, heads=3, layers=1)
+        axis = [i % 3 for i in range(rot // 2)]
+        spec = mv.RopeAxes(d, axis, 1e4)
+        n = 37
+        slot = p.reserve([0, 1], [0, 30, n])
+        wide = torch.randn(n, 10 * d, generator=p.gen).to(BF).cuda()
+        k, v = (wide[:, x * d:(x + 3) * d].view(n, 3, d) for x in (1, 6))
+        pos = torch.randint(0, 9000, (3, n), generator=p.gen).to(torch.int32).cuda()
+        slot[5], slot[36], slot[7] = -1, p.c.shape.n_pages * p.c.shape.page_size, -(2 ** 31)
+        rot_k = mv.rope_axes(k, pos, spec)
+        mv.cache_write(p.c, 0, slot, k, v, rope=spec, pos=pos)
+        p.m.write(0, slot.tolist(), rot_k.double().cpu().numpy(), v.double().cpu().numpy())
+        p.same()
+
+
+def test_refusals():
+    c = mv.PagedCache(1, 8, 16, 2, 64, 4, 4)
+    ids, ptr = i32([0, 1]), i32([0, 1, 2])
+    slot, _ = mv.cache_reserve(c, ids, ptr, 2)
+    k = torch.zeros(2, 2, 64, dtype=BF, device="cuda")
+    for bad in (lambda: mv.cache_reserve(c, ids.long(), ptr, 2),
+                lambda: mv.cache_reserve(c, ids, ptr[:2], 2),
+                lambda: mv.cache_reserve(c, ids.cpu(), ptr, 2),
+                lambda: mv.cache_write(c, 0, slot, k[:1], k),
+                lambda: mv.cache_write(c, 0, slot, k.float(), k),
+                lambda: mv.cache_write(c, 0, slot, k, k, rope=mv.RopeAxes(64, [0])),
+                lambda: mv.cache_write(c, 0, slot, k, k, rope=mv.RopeAxes(128, [0]),
+                                       pos=ptr.view(1, 3)),
+                lambda: mv.cache_fork(c, ids, ptr), lambda: mv.cache_free(c, ids.view(1, 2)),
+                lambda: mv.cache_compact(c, ids, ids, ptr, ptr)):
+        with pytest.raises(ValueError):
+            bad()
+    small = torch.empty(16, dtype=torch.uint8, device="cuda")
+    for bad in (lambda: mv.cache_write(c, 1, slot, k, k), lambda: mv.cache_write(c, -1, slot, k, k),
+                lambda: mv.cache_fork(c, ids, i32([2, 3]), workspace=small)):
+        with pytest.raises(mv.MVError):
+            bad()
+    for shape in ((1, 8, 24, 2, 64, 4, 4), (1, 8, 16, 2, 96, 4, 4), (1, 8, 16, 2, 64, 9000, 4),
+                  (0, 8, 16, 2, 64, 4, 4), (1, 1 << 27, 16, 2, 64, 4, 4)):
+        with pytest.raises(mv.MVError):
+            mv.PagedCache(*shape)
+    assert c.seq_len.tolist() == [1, 1, 0, 0]

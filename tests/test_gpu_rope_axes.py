@@ -1,0 +1,135 @@
+"""Rotary positions with several axes against the plain form in 64 bits.
+
+Tolerance: one rounding to bf16 (2^-8 of the result) after fp32 arithmetic.
+The angle is reduced in fp64: |angle| <= 2^31, its ulp 2^-22, the product's and
+the reduction's error below 2^-21; cos and sin of the fp32 angle in [-pi, pi]
+are then off by 2^-21 + 2^-23 (the angle's rounding) + 2^-22 (the function), so
+a rotated element by less than (|a| + |b|) 2^-19.  For positions up to 2^17
+the first term is below 2^-35 and 2^-20 bounds the sum."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache as OC
+from paper_2609_00865_amd import mv
+
+pytestmark = pytest.mark.gpu
+BF = torch.bfloat16
+
+
+def _case(n, H, d, axis, n_axes, seed, top=1 << 17):
+    gen = torch.Generator().manual_seed(seed)
+    x = torch.randn(n, H, d, generator=gen).to(BF)
+    pos = torch.randint(-top, top, (n_axes, n), generator=gen, dtype=torch.int64).to(torch.int32)
+    return x, pos
+
+
+def _check(got, x, pos, axis, theta, inverse, eps=2.0 ** -20):
+    x64 = x.double().numpy()
+    ref = OC.rotate(x64, pos.numpy(), axis, theta, inverse)
+    P = len(axis)
+    mag = np.abs(x64)
+    both = mag[..., :P] + mag[..., P:2 * P]
+    slack = np.concatenate([both, both, 0 * mag[..., 2 * P:]], -1) * eps
+    err = np.abs(got.double().cpu().numpy() - ref)
+    assert (err <= 2.0 ** -8 * (np.abs(ref) + slack) + slack).all(), err.max()
+    assert torch.equal(got.cpu()[..., 2 * P:], x[..., 2 * P:])
+
+
+AXES = {"one": lambda P: [0] * P,
+        "runs": lambda P: [0] * (P // 4) + [1] * ((P - P // 4) // 2)
+        + [2] * (P - P // 4 - (P - P // 4) // 2),
+        "turns": lambda P: [i % 3 for i in range(P)],
+        "eight": lambda P: [(5 * i + i // 7) % 8 for i in range(P)]}
+
+
+@pytest.mark.parametrize("n,H,d,rot", [(1, 1, 64, 64), (5, 3, 128, 128), (257, 2, 80, 80),
+                                       (33, 4, 80, 40), (7, 2, 96, 94), (64, 5, 128, 2),
+                                       (3, 1, 8, 6), (4099, 3, 64, 32), (19, 2, 256, 256)])
+@pytest.mark.parametrize("axes", sorted(AXES))
+def test_rotation(n, H, d, rot, axes):
+    axis = AXES[axes](rot // 2)
+    x, pos = _case(n, H, d, axis, 8, n + rot)
+    spec = mv.RopeAxes(d, axis, 1e4)
+    pos = pos[:spec.n_axes].contiguous()
+    print(f"[gpu] rope axes n={n} H={H} d={d} rot={rot} {axes}", flush=True)
+    for inverse in (False, True):
+        got = mv.rope_axes(x.cuda(), pos.cuda(), spec, inverse=inverse)
+        _check(got, x, pos, axis, spec.theta, inverse)
+
+
+@pytest.mark.parametrize("n", [1, 37, 4500])
+def test_strided_and_in_place(n):
+    """A slice of a fused projection, rotated into another, and in place; what
+    lies beside the slice stays."""
+    H, d, wide = 3, 64, 5 * 64 + 8
+    axis = AXES["turns"](d // 2)
+    spec = mv.RopeAxes(d, axis, 1e6)
+    gen = torch.Generator().manual_seed(n)
+    buf = torch.randn(n, wide, generator=gen).to(BF).cuda()
+    pos = torch.randint(0, 5000, (3, n), generator=gen).to(torch.int32).cuda()
+    x = buf[:, 64:64 + H * d].view(n, H, d)
+    ref = mv.rope_axes(x.contiguous(), pos, spec)
+    other = torch.full((n, wide), 7.0, dtype=BF, device="cuda")
+    out = other[:, 8:8 + H * d].view(n, H, d)
+    assert mv.rope_axes(x, pos, spec, out=out) is out
+    assert torch.equal(out, ref)
+    assert (other[:, :8] == 7).all() and (other[:, 8 + H * d:] == 7).all()
+    before = buf.clone()
+    mv.rope_axes(x, pos, spec, out=x)
+    torch.cuda.synchronize()
+    assert torch.equal(x, ref)
+    assert torch.equal(buf[:, :64], before[:, :64])
+    assert torch.equal(buf[:, 64 + H * d:], before[:, 64 + H * d:])
+
+
+def test_far_positions():
+    """The whole int32 range of positions."""
+    x, _ = _case(64, 2, 128, None, 1, 5)
+    axis = [0] * 64
+    pos = torch.linspace(-2 ** 31, 2 ** 31 - 1, 64, dtype=torch.float64).to(torch.int32)[None]
+    spec = mv.RopeAxes(128, axis, 1e6)
+    for inverse in (False, True):
+        _check(mv.rope_axes(x.cuda(), pos.contiguous().cuda(), spec, inverse=inverse), x, pos, axis, spec.theta,
+               inverse, eps=2.0 ** -19)
+
+
+def test_inverse_is_the_gradient():
+    """<R x, g> = <x, R^-1 g>, and the gradient by differences: R is linear, so
+    R(x + h e) - R(x) = h R e, exactly up to the roundings of both sides."""
+    n, H, d = 23, 2, 64
+    axis = AXES["runs"](d // 2)
+    spec = mv.RopeAxes(d, axis, 1e4)
+    x, pos = _case(n, H, d, axis, 3, 1)
+    g, _ = _case(n, H, d, axis, 3, 2)
+    y = mv.rope_axes(x.cuda(), pos.cuda(), spec).double().cpu()
+    dx = mv.rope_axes(g.cuda(), pos.cuda(), spec, inverse=True).double().cpu()
+    a, b = (y * g.double()).sum(), (x.double() * dx).sum()
+    # each product carries one rounding of its output
+    bound = 2.0 ** -8 * ((y * g.double()).abs().sum() + (x.double() * dx).abs().sum()) + 1e-3
+    assert abs(float(a - b)) <= float(bound)
+    for t, h, e in ((0, 0, 3), (22, 1, 40), (11, 0, 63)):
+        step = torch.zeros_like(x)
+        step[t, h, e] = 1.0
+        col = mv.rope_axes(step.cuda(), pos.cuda(), spec).double().cpu()
+        lhs, rhs = float((col * g.double()).sum()), float(dx[t, h, e])
+        assert abs(lhs - rhs) <= 2.0 ** -8 * (float((col * g.double()).abs().sum()) + abs(rhs)) + 1e-4
+
+
+def test_refusals():
+    spec = mv.RopeAxes(64, [0] * 32)
+    x = torch.zeros(4, 2, 64, dtype=BF, device="cuda")
+    pos = torch.zeros(1, 4, dtype=torch.int32, device="cuda")
+    for bad in (lambda: mv.rope_axes(x.float(), pos, spec), lambda: mv.rope_axes(x.cpu(), pos, spec),
+                lambda: mv.rope_axes(x[:, :, :32], pos, spec),
+                lambda: mv.rope_axes(x.transpose(0, 1), pos, spec),
+                lambda: mv.rope_axes(x, pos.long(), spec), lambda: mv.rope_axes(x, pos[:, :3], spec),
+                lambda: mv.rope_axes(x, pos, mv.RopeAxes(64, [0, 1])),
+                lambda: mv.rope_axes(x, pos, spec, out=torch.empty_like(x)[:3])):
+        with pytest.raises(ValueError):
+            bad()
+    wide = torch.zeros(4, 132, dtype=BF, device="cuda")
+    with pytest.raises(mv.MVError, match="stride"):
+        mv.rope_axes(wide[:, :128].view(4, 2, 64), pos, spec)
+    empty = mv.rope_axes(x[:0], pos[:, :0], spec)
+    assert empty.shape == (0, 2, 64)

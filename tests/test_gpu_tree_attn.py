@@ -1,0 +1,397 @@
+"""Attention over the cache against the plain form in 64 bits.
+
+Tolerance of o, element by element: its rounding to bf16 (2^-8 |o|), the
+rounding of the probabilities to bf16 (each by at most 2^-8 of itself, so
+2^-8 sum w |v|), and the scores' error: fp32 sums of d products, off by at
+most d 2^-24 sum |q k| scale =: e, as a relative error 2 e of the weights (both
+sides of the quotient), L 2^-24 for fp32 sums of L terms and 2^-20 for the
+exponential (its argument's rounding is inside e: |score| 2^-24 of it).  lse:
+e, the same sums, and its rounding.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import cache as OC
+from paper_2609_00865_amd import mv
+
+pytestmark = pytest.mark.gpu
+BF = torch.bfloat16
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+class Setup:
+    """A cache whose sequences have the given lengths on scattered pages, and q
+    of the given new rows."""
+
+    def __init__(self, lens, rows, hq, hkv, d, page=16, seed=0, ids=None, layers=1, layer=0,
+                 stale=None, spread=1.0):
+        rng = np.random.default_rng(seed)
+        gen = torch.Generator().manual_seed(seed)
+        need = [-(-n // page) for n in lens]
+        pages = sum(need) + 3
+        order = rng.permutation(pages).tolist()
+        table = [[order.pop() for _ in range(n)] for n in need]
+        wide = max(need + [1]) + 2
+        shape = (layers, pages, hkv, page, d)
+        self.k, self.v = (torch.randn(shape, generator=gen).to(BF) for _ in range(2))
+        if spread != 1.0:
+            self.k *= spread
+        self.lens, self.table, self.page, self.layer = lens, table, page, layer
+        self.rows, self.ids = rows, list(range(len(lens))) if ids is None else ids
+        N = sum(rows)
+        self.q = torch.randn(N, hq, d, generator=gen).to(BF)
+        if stale is not None:      # every row that no sequence holds
+            live = torch.zeros(pages, page, dtype=torch.bool)
+            for t, n in zip(table, lens):
+                for r in range(n):
+                    live[t[r // page], r % page] = True
+            dead = ~live[None, :, None, :, None].expand(shape)
+            self.k[dead], self.v[dead] = stale, stale
+        self.dev(wide)
+
+    def dev(self, wide):
+        L, pages, hkv, page, d = self.k.shape
+        self.c = mv.PagedCache(L, pages, page, hkv, d, len(self.lens), wide)
+        self.c.k.copy_(self.k)
+        self.c.v.copy_(self.v)
+        refs = [0] * pages
+        for t in self.table:
+            for p in t:
+                refs[p] = 1
+        self.c.restore(i32([t + [-1] * (wide - len(t)) for t in self.table]), i32(self.lens),
+                       i32(refs))
+
+    def ptr(self):
+        return [0] + np.cumsum(self.rows).tolist()
+
+    def run(self, tree=None, **kw):
+        return mv.tree_attn(self.c, self.layer, self.q.cuda(), i32(self.ids), i32(self.ptr()),
+                            tree=tree, **kw)
+
+    def rows_of(self, s):
+        n = self.lens[s]
+        at = [(self.table[s][r // self.page], r % self.page) for r in range(n)]
+        k = torch.stack([self.k[self.layer, p, :, r] for p, r in at]) if n else None
+        v = torch.stack([self.v[self.layer, p, :, r] for p, r in at]) if n else None
+        return k, v
+
+    def check(self, o, lse, see_new=None, scale=None, skip=()):
+        """see_new(b, n): [n, n] bool of the new rows each row sees."""
+        d = self.q.shape[2]
+        scale = 1.0 / math.sqrt(d) if scale is None else scale
+        at = 0
+        for b, (s, n) in enumerate(zip(self.ids, self.rows)):
+            r = slice(at, at + n)
+            at += n
+            if n == 0 or b in skip:
+                continue
+            go, gl = o[r].double().cpu().numpy(), lse[:, r].double().cpu().numpy()
+            L = self.lens[s] if 0 <= s < len(self.lens) else 0
+            if L == 0:
+                assert (go == 0).all() and np.isneginf(gl).all()
+                continue
+            new = np.tril(np.ones((n, n), dtype=bool)) if see_new is None else see_new(b, n)
+            see = np.ones((n, L), dtype=bool)
+            c = L - n
+            for i in range(n):
+                for j in range(n):
+                    if c + j >= 0:
+                        see[i, c + j] = new[i, j]
+            k, v = (x.double().numpy() for x in self.rows_of(s))
+            q = self.q[r].double().numpy()
+            with np.errstate(invalid="ignore"):
+                ro, rl, mag = OC.attend(k, v, q, see, scale)
+            g = q.shape[1] // k.shape[1]
+            kf = np.where(np.isfinite(k), np.abs(k), 0).max(0)           # [hkv, d]
+            e = d * 2.0 ** -24 * scale * np.stack([np.abs(q[:, h]) @ kf[h // g]
+                                                   for h in range(q.shape[1])], 1)   # [n, hq]
+            rel = 2.0 ** -8 + 2 * e + L * 2.0 ** -24 + 2.0 ** -20
+            bound = 2.0 ** -8 * np.abs(ro) + 1.01 * rel[..., None] * mag + 1e-30
+            fin = np.isfinite(ro)
+            assert (np.isnan(go) == np.isnan(ro)).all(), (b, "NaN where the plain form has none, or not")
+            assert (go[~fin & ~np.isnan(ro)] == ro[~fin & ~np.isnan(ro)]).all()
+            err = np.abs(go - ro)[fin]
+            assert (err <= bound[fin]).all(), (b, s, float((err - bound[fin]).max()))
+            lb = e.T + L * 2.0 ** -24 + 2.0 ** -20 + 2.0 ** -22 * np.abs(np.where(np.isfinite(rl), rl, 0))
+            lf = np.isfinite(rl)
+            assert (np.isneginf(gl) == np.isneginf(rl)).all()
+            assert (np.abs(gl - rl)[lf] <= lb[lf]).all(), float((np.abs(gl - rl) - lb)[lf].max())
+
+
+def parents(rng, n):
+    return [int(rng.integers(max(-1, i - 5), i)) for i in range(n)]
+
+
+HEADS = [(1, 1), (4, 4), (7, 1), (28, 4), (40, 1), (66, 2)]
+
+
+@pytest.mark.parametrize("hq,hkv", HEADS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("page", [16, 64])
+def test_single_tokens(hq, hkv, d, page):
+    """One row each, over 1 key, tile and page ends and a few thousand keys."""
+    lens = [1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 257, 700, 2311]
+    s = Setup(lens, [1] * len(lens), hq, hkv, d, page, seed=hq + d)
+    print(f"[gpu] single tokens {hq}/{hkv} d={d} page={page}", flush=True)
+    s.check(*s.run())
+    s.check(*s.run(max_len=max(lens)))
+
+
+@pytest.mark.parametrize("rows", [[1], [2, 3], [7, 1, 33], [64, 0, 5, 65], [129], [300, 17]])
+@pytest.mark.parametrize("d,hq,hkv", [(128, 7, 1), (64, 8, 2)])
+def test_chunks(rows, d, hq, hkv):
+    """Several rows over their context, a row without context first (a
+    sequence just begun), and an entry of no rows."""
+    ctx = [0, 5, 64, 200][:len(rows)] if len(rows) > 1 else [71]
+    s = Setup([a + b for a, b in zip(ctx, rows)], rows, hq, hkv, d, 32, seed=len(rows))
+    print(f"[gpu] chunks {rows} d={d}", flush=True)
+    s.check(*s.run())
+    s.check(*s.run(scale=0.3), scale=0.3)
+
+
+@pytest.mark.parametrize("rows,ctx", [([1], [40]), ([5, 12], [0, 33]), ([33, 64, 7], [100, 1, 64]),
+                                      ([95, 31, 32], [500, 250, 31]), ([200], [63])])
+@pytest.mark.parametrize("d,hq,hkv", [(128, 14, 2), (64, 3, 3)])
+def test_trees(rows, ctx, d, hq, hkv):
+    rng = np.random.default_rng(sum(rows))
+    s = Setup([a + b for a, b in zip(ctx, rows)], rows, hq, hkv, d, 16, seed=7)
+    par = [parents(rng, n) for n in rows]
+    print(f"[gpu] trees {rows} over {ctx} d={d}", flush=True)
+    tree, depth = mv.tree_mask(i32([x for p in par for x in p]), i32(s.ptr()), max(rows))
+    seen = [OC.tree_rows(p, len(p)) for p in par]
+    assert depth.tolist() == [x for _, dep in seen for x in dep]
+    words = tree.cpu().numpy().view(np.uint32)
+    at = 0
+    for see, _ in seen:
+        n = len(see)
+        bits = (words[at:at + n, :, None] >> np.arange(32, dtype=np.uint32)) & 1
+        assert np.array_equal(bits.reshape(n, -1)[:, :n].astype(bool), see)
+        assert not bits.reshape(n, -1)[:, n:].any()
+        at += n
+    s.check(*s.run(tree), see_new=lambda b, n: seen[b][0])
+
+
+def test_tree_mask_edges():
+    """Parents that are no earlier row make roots; words past max_rows have no
+    bits; rows after the last entry are left alone."""
+    par = [-1, 0, 2, 5, -7, 3, 2 ** 31 - 1, -1, 0, 1, 2]
+    tree, depth = mv.tree_mask(i32(par), i32([0, 7, 11]), 3)
+    ref = [OC.tree_rows(par[:7], 7), OC.tree_rows(par[7:], 4)]
+    assert depth.tolist() == ref[0][1] + ref[1][1]
+    assert tree[:, 0].tolist() == [sum(1 << j for j in range(len(r)) if r[j])
+                                   for see, _ in ref for r in see]
+    n = 100
+    chain = [i - 1 for i in range(n)]
+    tree, depth = mv.tree_mask(i32(chain), i32([0, n]), 40)     # 2 words for 100 rows
+    assert depth.tolist() == list(range(n)) and tree.shape == (n, 2)
+    w = tree.cpu().numpy().view(np.uint32)
+    for i in range(n):
+        full = (1 << (i + 1)) - 1
+        assert int(w[i, 0]) == full & 0xffffffff and int(w[i, 1]) == (full >> 32) & 0xffffffff
+    tree, depth = mv.tree_mask(i32(chain), i32([0, 60]), 60)
+    torch.cuda.synchronize()
+    assert depth[:60].tolist() == list(range(60))
+
+
+def test_rows_that_see_nothing():
+    """Masks of a row's own bits: rows with none, over an empty context, give
+    0 and -inf; sequences shorter than their entry; padded and bad ids; a
+    sequence named twice."""
+    rows, lens = [4, 3, 5, 2, 1, 3], [4, 1, 40, 0]
+    ids = [0, 1, 2, 3, -1, 2]
+    s = Setup(lens, rows, 6, 2, 64, 16, seed=3, ids=ids)
+    N = sum(rows)
+    words = np.zeros((N, 1), dtype=np.int32)
+    see = [np.zeros((n, n), dtype=bool) for n in rows]
+    see[0][1, [0, 3]] = see[0][2, 2] = True              # row 1 sees a later row; 0 and 3 nothing
+    see[1][:] = True                                     # two of three rows are not in the cache
+    see[2][4, 0] = True                                  # the others: the context alone
+    see[5][1, 1] = True
+    at = 0
+    for x in see:
+        for r in x:
+            words[at, 0] = sum(1 << j for j in np.flatnonzero(r))
+            at += 1
+    o, lse = s.run(torch.from_numpy(words).cuda())
+    s.check(o, lse, see_new=lambda b, n: see[b])
+    assert (o[0] == 0).all() and torch.isneginf(lse[:, 0]).all() and (o[3] == 0).all()
+    assert (o[14:15] == 0).all() and torch.isneginf(lse[:, 14]).all()
+    s.check(*s.run())                                    # the chain over the same
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf"), 3e38])
+@pytest.mark.parametrize("d", [64, 128])
+def test_unseen_rows_do_not_show(bad, d):
+    """Whatever stands in rows past the end and in drafted rows that a row does
+    not see, finite or not; where it is seen, it shows as in the plain form."""
+    rng = np.random.default_rng(11)
+    rows, ctx = [6, 40, 1, 3], [50, 0, 31, 30]
+    s = Setup([a + b for a, b in zip(ctx, rows)], rows, 6, 2, d, 16, seed=2, stale=bad)
+    par = [parents(rng, n) for n in rows]
+    seen = [OC.tree_rows(p, len(p))[0] for p in par]
+    tree, _ = mv.tree_mask(i32([x for p in par for x in p]), i32(s.ptr()), max(rows))
+    print(f"[gpu] unseen rows {bad} d={d}", flush=True)
+    o, lse = s.run(tree)
+    assert torch.isfinite(o.float()).all() and torch.isfinite(lse).all()
+    s.check(o, lse, see_new=lambda b, n: seen[b])
+    for b, a in ((0, 2), (1, 17), (1, 39), (3, 1)):      # drafted rows themselves
+        r = s.lens[b] - rows[b] + a
+        p, x = s.table[b][r // 16], r % 16
+        s.v[0, p, 0, x, 5] = bad
+        if b == 1:
+            s.k[0, p, 1, x, 9] = bad
+    s.dev(s.c.shape.max_pages)
+    big = abs(bad) == 3e38
+    o, lse = s.run(tree)
+    if not big:
+        s.check(o, lse, see_new=lambda b, n: seen[b])
+    g, at = 3, 0
+    for b, n in enumerate(rows):
+        for i in range(n):
+            sees = any(b == bb and seen[b][i, a] for bb, a in ((0, 2), (1, 17), (1, 39), (3, 1)))
+            if not sees:
+                assert torch.isfinite(o[at + i].float()).all(), (b, i)
+        at += n
+
+
+def test_a_context_that_is_not_finite():
+    """NaN in a key that is seen makes the row NaN, not empty."""
+    s = Setup([40, 33], [1, 2], 4, 2, 64, 16, seed=5)
+    s.k[0, s.table[0][0], 0, 3, 0] = float("nan")
+    s.dev(s.c.shape.max_pages)
+    o, lse = s.run()
+    assert torch.isnan(o[0, :2].float()).all() and torch.isnan(lse[:2, 0]).all()
+    assert torch.isfinite(o[0, 2:].float()).all() and torch.isfinite(o[1:].float()).all()
+    one = Setup([1], [1], 1, 1, 64, 16, seed=5)
+    one.k[0, one.table[0][0], 0, 0, 0] = float("nan")
+    one.dev(one.c.shape.max_pages)
+    o, lse = one.run()
+    assert torch.isnan(o.float()).all() and torch.isnan(lse).all()
+
+
+def test_large_scores():
+    """Scores in the hundreds, growing along the keys: every tile moves the maximum."""
+    s = Setup([900, 333], [1, 40], 8, 2, 128, 16, seed=9, spread=20.0)
+    for b in range(2):
+        for r in range(s.lens[b]):
+            s.k[0, s.table[b][r // 16], :, r % 16] *= 1 + r / 300
+    s.dev(s.c.shape.max_pages)
+    s.check(*s.run())
+
+
+def test_uneven_batch():
+    """One long sequence among short ones, and more entries than fit the
+    sizes held on chip."""
+    lens = [9000] + [1 + (i * 37) % 90 for i in range(40)]
+    s = Setup(lens, [1] * 41, 7, 1, 64, 16, seed=1)
+    s.check(*s.run())
+    B = 1500
+    lens = [1 + (i * 53) % 20 for i in range(B)]
+    rows = [min(n, 1 + i % 2) for i, n in enumerate(lens)]
+    s = Setup(lens, rows, 2, 1, 64, 16, seed=2)
+    print(f"[gpu] {B} entries", flush=True)
+    s.check(*s.run())
+    s.check(*s.run(max_len=20))
+
+
+def test_hint_is_only_a_hint():
+    """max_len shorter than the sequences changes how the work is cut, not the result."""
+    s = Setup([5000, 300, 1], [1, 9, 1], 14, 2, 128, 64, seed=4)
+    for m in (0, 1, 64, 5000, 2 ** 31 - 1):
+        s.check(*s.run(max_len=m))
+
+
+def test_rows_behind_the_last_entry_stay():
+    s = Setup([30, 20], [3, 2], 4, 2, 64, 16, seed=1)
+    q = torch.cat([s.q, torch.randn(6, 4, 64).to(BF)]).cuda()
+    o = torch.full_like(q, 5.0)
+    lse = torch.full((4, 11), 5.0, device="cuda")
+    mv.tree_attn(s.c, 0, q, i32([0, 1]), i32([0, 3, 5]), out=(o, lse))
+    torch.cuda.synchronize()
+    assert (o[5:] == 5).all() and (lse[:, 5:] == 5).all()
+    s.check(o[:5], lse[:, :5])
+    tree = torch.full((11, 1), -1, dtype=torch.int32, device="cuda")
+    mv.tree_attn(s.c, 0, q, i32([0, 1]), i32([0, 3, 5]), tree=tree, out=(o, lse))
+    s.check(o[:5], lse[:, :5], see_new=lambda b, n: np.ones((n, n), dtype=bool))
+
+
+def test_layers_and_far_offsets():
+    """A layer behind 2^32 bytes, and pages behind 2^31 elements of one layer."""
+    hkv, d, page = 8, 128, 256
+    pages = 8300                                   # 2.18e9 elements a layer, 4.4 GB
+    c = mv.PagedCache(2, pages, page, hkv, d, 2, 4)
+    gen = torch.Generator().manual_seed(1)
+    n = [700, 300]
+    table = [[8299, 5, 8200], [8298, 0]]
+    rows = [[torch.randn(m, hkv, d, generator=gen).to(BF) for _ in range(2)] for m in n]
+    refs = torch.zeros(pages, dtype=torch.int32)
+    for t in table:
+        refs[torch.tensor(t)] = 1
+    c.restore(i32([t + [-1] * (4 - len(t)) for t in table]), i32(n), refs.cuda())
+    for s in range(2):
+        slot = i32([table[s][r // page] * page + r % page for r in range(n[s])])
+        mv.cache_write(c, 1, slot, rows[s][0].cuda(), rows[s][1].cuda())
+    q = torch.randn(4, 8, d, generator=gen).to(BF)
+    print("[gpu] far offsets", flush=True)
+    o, lse = mv.tree_attn(c, 1, q.cuda(), i32([0, 1]), i32([0, 1, 4]))
+    at = 0
+    for s, m in ((0, 1), (1, 3)):
+        see = np.ones((m, n[s]), dtype=bool)
+        see[:, n[s] - m:] = np.tril(np.ones((m, m), dtype=bool))
+        k, v = (x.double().numpy() for x in rows[s])
+        ro, rl, mag = OC.attend(k, v, q[at:at + m].double().numpy(), see, 1 / math.sqrt(d))
+        err = np.abs(o[at:at + m].double().cpu().numpy() - ro)
+        assert (err <= 2.0 ** -8 * (np.abs(ro) + 1.05 * mag) + 1e-3 * mag).all()
+        at += m
+    mv.cache_compact(c, i32([0]), i32([0]), i32([0, 1]), i32([[10, 600]]))
+    o2, _ = mv.tree_attn(c, 1, q[:1].cuda(), i32([0]), i32([0, 1]))
+    k, v = (np.delete(x.double().numpy(), np.arange(10, 600), 0) for x in rows[0])
+    ro, _, mag = OC.attend(k, v, q[:1].double().numpy(), np.ones((1, 110), dtype=bool),
+                           1 / math.sqrt(d))
+    err = np.abs(o2.double().cpu().numpy() - ro)
+    assert (err <= 2.0 ** -8 * (np.abs(ro) + 1.05 * mag) + 1e-3 * mag).all()
+
+
+def test_same_result_every_time_and_on_another_stream():
+    s = Setup([3000, 40, 800], [1, 17, 5], 28, 4, 128, 16, seed=6)
+    o, lse = s.run()
+    q, ids, ptr = s.q.cuda(), i32(s.ids), i32(s.ptr())
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    o2, lse2 = mv.tree_attn(s.c, 0, q, ids, ptr, stream=side)
+    with torch.cuda.stream(side):
+        o3, lse3 = mv.tree_attn(s.c, 0, q, ids, ptr)
+    torch.cuda.synchronize()
+    for a, b in ((o2, lse2), (o3, lse3)):
+        assert torch.equal(o, a) and torch.equal(lse, b)
+
+
+def test_refusals():
+    s = Setup([30, 20], [3, 2], 4, 2, 64, 16, seed=1)
+    q, ids, ptr = s.q.cuda(), i32([0, 1]), i32([0, 3, 5])
+    tree = torch.zeros(5, 1, dtype=torch.int32, device="cuda")
+    for bad in (lambda: mv.tree_attn(s.c, 0, q.float(), ids, ptr),
+                lambda: mv.tree_attn(s.c, 0, q[..., :32].contiguous(), ids, ptr),
+                lambda: mv.tree_attn(s.c, 0, q, ids, ptr[:2]),
+                lambda: mv.tree_attn(s.c, 0, q, ids.long(), ptr),
+                lambda: mv.tree_attn(s.c, 0, q, ids, ptr, tree=tree[:4]),
+                lambda: mv.tree_attn(s.c, 0, q, ids, ptr, tree=tree[:, :0].contiguous()),
+                lambda: mv.tree_attn(s.c, 0, q, ids, ptr, out=(q[:3], q)),
+                lambda: mv.tree_mask(ptr.float(), ptr, 3)):
+        with pytest.raises(ValueError):
+            bad()
+    small = torch.empty(1024, dtype=torch.uint8, device="cuda")
+    for bad in (lambda: mv.tree_attn(s.c, 1, q, ids, ptr),
+                lambda: mv.tree_attn(s.c, 0, q[:, :3].contiguous(), ids, ptr),
+                lambda: mv.tree_attn(s.c, 0, q, ids, ptr, workspace=small),
+                lambda: mv.tree_attn(s.c, 0, q, ids, ptr, scale=float("nan"))):
+        with pytest.raises(mv.MVError):
+            bad()
+    o, lse = mv.tree_attn(s.c, 0, q[:0], ids[:0], ptr[:1])
+    assert o.shape == (0, 4, 64) and lse.shape == (4, 0)
