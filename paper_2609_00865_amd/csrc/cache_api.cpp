@@ -27,7 +27,7 @@ hipError_t launch_cache_move(const mv_cache_shape& shape, const CacheDev& a, int
                              hipStream_t stream);
 hipError_t launch_cache_free(const CacheDev& a, int n, const int32_t* ids, hipStream_t stream);
 size_t tree_attn_ws_bytes(const mv_cache_shape& c, const mv_tree_attn_shape& s);
-int64_t tree_attn_blocks(const mv_cache_shape& c, const mv_tree_attn_shape& s);
+bool tree_attn_fits(const mv_cache_shape& c, const mv_tree_attn_shape& s);
 hipError_t launch_tree_attn(const mv_cache_shape& cs, const CacheDev& cd, int layer,
                             const mv_tree_attn_shape& s, float scale, const int32_t* ids,
                             const int32_t* ptr, const uint32_t* tree, const void* q, void* o,
@@ -147,9 +147,8 @@ mv_status check_tree_shape(const mv_cache_shape* c, const mv_tree_attn_shape* s)
   if (s->n_heads_q <= 0 || s->n_heads_q % c->n_heads_kv != 0)
     return fail(MV_ERR_SHAPE, "n_heads_q must be a positive multiple of n_heads_kv");
   if (!std::isfinite(s->softmax_scale)) return fail(MV_ERR_INVALID_ARG, "softmax_scale not finite");
-  if (int64_t(s->n_rows) * s->n_heads_q >= (int64_t(1) << 30) ||
-      mv::tree_attn_blocks(*c, *s) >= (int64_t(1) << 30))
-    return fail(MV_ERR_UNSUPPORTED, "n_rows * n_heads_q must stay below 2^30");
+  if (int64_t(s->n_rows) * s->n_heads_q >= (int64_t(1) << 30) || !mv::tree_attn_fits(*c, *s))
+    return fail(MV_ERR_UNSUPPORTED, "too many rows in one call");
   return MV_OK;
 }
 

@@ -1,18 +1,26 @@
 // Attention of a sequence's newest rows (one decoded token, a tree of drafted
 // ones, a chunk of a prompt) over its rows in a paged cache, on gfx950.
 //
-// A tile is up to 32 (query row, query head) pairs of one KV head: they read
-// the same keys.  A workgroup takes a tile's run of 64-key units; its waves
-// take 32-key tiles of that run in turn, each with K and V of its own in LDS
-// (two buffers, filled by direct loads a tile ahead, no barrier between
-// waves), S^T = K Q^T and O^T += V^T P^T with bf16 MFMA (a query per lane, so
-// the softmax statistics stay in a lane pair) and a running maximum and sum in
-// fp32; the waves' results meet in LDS.
+// A tile is R (query row, query head) pairs of one KV head, which read the
+// same keys; 64 keys of a tile are a unit of work.  The units of all tiles and
+// KV heads, one after another, are dealt to the workgroups in equal runs,
+// from the sequences' lengths as the device holds them: the workgroups do
+// equal work however uneven the batch is, with no copy to the host.  A run is
+// a few segments, each of one tile; a segment that is not its whole tile
+// leaves an unnormalised O with its maximum and sum, and a second pass joins
+// those of a tile in order.
 //
-// With few tiles the work is the reading of long caches, so every tile's
-// units are cut into runs of one common length, chosen on the device from
-// the sequences' lengths: the workgroups then do equal work however uneven
-// the batch is, and a second pass joins the runs of a tile in order.
+// Two kernels take a segment.  For few pairs (tree_few_kernel, R = 32) the
+// time is the reading of K and V: each wave streams 32-key tiles of its own
+// through its own LDS buffers, no barrier between waves, and the waves'
+// results meet in LDS at the end.  For many pairs (tree_many_kernel, R = 128)
+// the products count: four waves of 32 pairs share 64-key tiles, and the
+// scores of a tile are computed while the vector ALU turns those of the one
+// before into probabilities.  Both compute S^T = K Q^T and O^T += V^T P^T with
+// bf16 MFMA (a query per lane: the softmax statistics stay in a lane pair)
+// and keep maximum, sum and O in fp32.
+#include <type_traits>
+
 #include "mv_cache_dev.h"
 
 namespace mv {
@@ -23,8 +31,9 @@ struct TreeArgs {
   const u16* v;
   u16* o;
   float* lse;
-  float* part_o;       // [slots][R][D] unnormalised
-  float* part_ml;      // [slots][R][2] maximum (base 2, scaled), sum
+  float* part_o;       // [2 * groups][R][D] unnormalised
+  float* part_ml;      // [2 * groups][R][2] maximum (base 2, scaled), sum
+  int64_t* plan;       // [1 + tiles]: units of a KV head, then each place's first unit
   const int32_t* table;
   const int32_t* len;
   const int32_t* ids;
@@ -33,19 +42,26 @@ struct TreeArgs {
   int words;
   int B, N, Hq, Hkv, G, n_pages, n_seqs, max_pages, psl;
   int tiles;           // tile places: at least as many as there are tiles
-  int target;          // runs aimed at, over all KV heads
+  int groups;          // workgroups
   float scale_log2;
 };
 
-constexpr int kUnit = 64;      // keys of a unit of work
-constexpr int kPlanB = 1024;   // entries whose sizes are held in LDS
+constexpr int kUnit = 64;       // keys of a unit of work
+constexpr int kPlanB = 512;     // entries whose sizes are held in LDS
+constexpr int kChunks = 256;    // blocks of tile places whose first unit is held in LDS
 
 struct TreeShared {
   int ptr[kPlanB + 1];
   int len[kPlanB];
   int tmp[17];
-  int found[4];
+  int64_t first[kChunks + 1];   // first unit of each BLOCK of places
+  int pre[257];                 // of one of them: each place's first unit, from there
 };
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  return int64_t(uint64_t(uint32_t(uniform(int(x >> 32)))) << 32 | uint32_t(uniform(int(x))));
+}
 
 // One tile: the entry, its first pair, and the keys any of its rows may see.
 struct Tile {
@@ -53,6 +69,10 @@ struct Tile {
   int r0;           // its first row of q
   int m0, rows;     // first pair and pairs of the tile (0: no such tile)
   int kmax;         // keys [0, kmax)
+  // a tile without keys is one unit: its rows are still written
+  __device__ __forceinline__ int units() const {
+    return rows ? max(1, (kmax + kUnit - 1) / kUnit) : 0;
+  }
 };
 
 // Entry b's first tile place: places of entries never overlap, because
@@ -60,6 +80,12 @@ struct Tile {
 template <int R>
 __device__ __forceinline__ int first_place(int64_t r, int b, int G) {
   return int(r * G / R) + b;
+}
+
+__device__ __forceinline__ int entry_len(const TreeArgs& a, int b) {
+  const int id = a.ids[b];
+  return unsigned(id) < unsigned(a.n_seqs)
+             ? int(min(int64_t(max(a.len[id], 0)), int64_t(a.max_pages) << a.psl)) : 0;
 }
 
 template <int R>
@@ -82,52 +108,95 @@ __device__ __forceinline__ Tile tile_of(const TreeArgs& a, const TreeShared& s, 
     t.rows = 0;
     return t;
   }
-  int L;
-  if (lds) {
-    L = s.len[lo];
-  } else {
-    const int id = a.ids[lo];
-    L = unsigned(id) < unsigned(a.n_seqs)
-            ? int(min(int64_t(max(a.len[id], 0)), int64_t(a.max_pages) << a.psl)) : 0;
-  }
+  const int L = lds ? s.len[lo] : entry_len(a, lo);
   t.c = L - t.n;
   const int last = (t.m0 + t.rows - 1) / a.G;
   t.kmax = a.tree ? L : max(0, t.c + last + 1);
   return t;
 }
 
-__device__ __forceinline__ void load_sizes(const TreeArgs& a, TreeShared& s) {
-  if (a.B <= kPlanB) {
-    for (int b = threadIdx.x; b <= a.B; b += blockDim.x) {
-      s.ptr[b] = min(max(a.ptr[b], 0), a.N);
-      if (b < a.B) {
-        const int id = a.ids[b];
-        s.len[b] = unsigned(id) < unsigned(a.n_seqs)
-                       ? int(min(int64_t(max(a.len[id], 0)), int64_t(a.max_pages) << a.psl)) : 0;
-      }
-    }
-  }
-  __syncthreads();
+// A tile's fields are the same in every lane: held in scalar registers.
+__device__ __forceinline__ Tile uniform(const Tile& t) {
+  return {uniform(t.b), uniform(t.n), uniform(t.c), uniform(t.r0), uniform(t.m0), uniform(t.rows),
+          uniform(t.kmax)};
 }
 
-// The run length (in units) that cuts the tiles of all KV heads into about
-// `target` runs.  A tile without keys is one unit: its rows are still written.
+// The deal: every workgroup works out the same one from the lengths.
 template <int R, int BLOCK>
-__device__ __forceinline__ int run_length(const TreeArgs& a, TreeShared& s) {
-  int64_t sum = 0;
-  for (int u = threadIdx.x; u < a.tiles; u += BLOCK) {
-    const Tile t = tile_of<R>(a, s, u);
-    if (t.rows) sum += max(1, (t.kmax + kUnit - 1) / kUnit);
+struct Deal {
+  const TreeArgs& a;
+  TreeShared& s;
+  int chunk;           // the BLOCK of places that s.pre is of
+  int64_t units;       // of one KV head
+  int64_t per;         // of a workgroup
+
+  __device__ __forceinline__ int64_t scan(int j, int64_t first) {
+    const int u = j * BLOCK + threadIdx.x;
+    const int mine = u < a.tiles ? tile_of<R>(a, s, u).units() : 0;
+    int total;
+    // (a tile has fewer than 2^25 units: BLOCK of them do not pass 2^31 unless
+    // the caches are past any memory, in which case the rows are unspecified)
+    const int before = block_scan<BLOCK>(mine, s.tmp, total);
+    s.pre[threadIdx.x] = before;
+    if (threadIdx.x == 0) s.pre[BLOCK] = total;
+    if (blockIdx.x == 0 && u < a.tiles) a.plan[1 + u] = first + before;
+    chunk = j;
+    return first + total;
   }
-#pragma unroll
-  for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
-  __shared__ int64_t part[BLOCK / 64];
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
-  __syncthreads();
-  int64_t all = 0;
-#pragma unroll
-  for (int w = 0; w < BLOCK / 64; ++w) all += part[w];
-  return int(max(int64_t(1), (all * a.Hkv + a.target - 1) / a.target));
+
+  __device__ __forceinline__ Deal(const TreeArgs& args, TreeShared& sh) : a(args), s(sh) {
+    if (a.B <= kPlanB) {
+      for (int b = threadIdx.x; b <= a.B; b += BLOCK) {
+        s.ptr[b] = min(max(a.ptr[b], 0), a.N);
+        if (b < a.B) s.len[b] = entry_len(a, b);
+      }
+    }
+    __syncthreads();
+    const int chunks = (a.tiles + BLOCK - 1) / BLOCK;
+    int64_t sum = 0;
+    for (int j = 0; j < chunks; ++j) {
+      if (threadIdx.x == 0) s.first[j] = sum;
+      sum = scan(j, sum);
+    }
+    if (threadIdx.x == 0) s.first[chunks] = sum;
+    if (blockIdx.x == 0 && threadIdx.x == 0) a.plan[0] = sum;
+    units = uniform(sum);
+    per = max(int64_t(1), (units * a.Hkv + a.groups - 1) / a.groups);
+    __syncthreads();
+  }
+
+  // The place that holds unit p of a KV head, and which of its units that is.
+  __device__ __forceinline__ void find(int64_t p, int& place, int& unit) {
+    int lo = 0, hi = (a.tiles + BLOCK - 1) / BLOCK;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (s.first[mid] <= p) lo = mid; else hi = mid;
+    }
+    const int j = uniform(lo);
+    const int64_t first = s.first[j];
+    if (j != chunk) {
+      __syncthreads();
+      scan(j, first);
+      __syncthreads();
+    }
+    const int x = int(p - first);
+    lo = 0, hi = BLOCK;   // the last place whose first unit is not past x
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (s.pre[mid] <= x) lo = mid; else hi = mid;
+    }
+    place = uniform(j * BLOCK + lo);
+    unit = uniform(x - s.pre[lo]);
+  }
+};
+
+// Workgroups of an XCD (dealt to them in turn) take neighbouring runs: tiles
+// of one sequence and KV head meet in its L2.
+__device__ __forceinline__ int run_of_block(int groups) {
+  int xcd, local;
+  xcd_split(xcd, local);
+  const int full = groups / kNumXcd, more = groups % kNumXcd;
+  return xcd * full + min(xcd, more) + local;
 }
 
 // What a partial result with maximum m counts for beside maximum M.  Without
@@ -136,33 +205,8 @@ __device__ __forceinline__ float weight(float m, float M) {
   return m == -INFINITY ? 1.f : fast_exp2(m - M);
 }
 
-// The tile and run of workgroup w of a KV head: found[0] = tile place,
-// found[1] = run, found[2] = runs of the tile; found[0] = -1 past the last.
-// With by_tile, w is a tile place and found[1] the tile's first run among all.
-template <int R, int BLOCK>
-__device__ __forceinline__ void find_run(const TreeArgs& a, TreeShared& s, int run, int w,
-                                         bool by_tile) {
-  if (threadIdx.x == 0) s.found[0] = -1;
-  int before = 0;
-  for (int u0 = 0; u0 < a.tiles; u0 += BLOCK) {
-    const int u = u0 + threadIdx.x;
-    int mine = 0, total;
-    if (u < a.tiles) {
-      const Tile t = tile_of<R>(a, s, u);
-      if (t.rows) mine = (max(1, (t.kmax + kUnit - 1) / kUnit) + run - 1) / run;
-    }
-    const int first = before + block_scan<BLOCK>(mine, s.tmp, total);
-    if (by_tile ? u == w && mine > 0 : w >= first && w < first + mine) {
-      s.found[0] = u;
-      s.found[1] = by_tile ? first : w - first;
-      s.found[2] = mine;
-    }
-    before += total;
-  }
-  __syncthreads();
-}
-
-// The keys of [key0, key0 + 32) that new row i of a tile's entry sees, as bits.
+// The keys of [key0, key0 + 32) that new row i of a tile's entry sees, as
+// bits; row: its row of q.
 __device__ __forceinline__ uint32_t seen32(const TreeArgs& a, const Tile& t, int64_t row, int i,
                                            int key0) {
   auto low = [](int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u; };
@@ -181,307 +225,727 @@ __device__ __forceinline__ uint32_t seen32(const TreeArgs& a, const Tile& t, int
   return bits | low(t.c - key0);                 // and the context
 }
 
-// NW waves, each with two K and two V tiles of 32 keys.
+// Page ids of the keys ahead, per wave: 64 at a time into two LDS slots by
+// direct loads that land in order with those of the keys.
+struct PageRing {
+  const int32_t* row;   // the sequence's table
+  uint32_t lds;         // slot 0 (slot 1 is 256 bytes behind)
+  const int* slots;
+  int window;           // the last window asked for
+  int n_pages, psl;
+  __device__ __forceinline__ void load(int w, int last_page) {
+    // lanes past the last page read it again
+    const int lane = threadIdx.x & 63;
+    lds_load4(row + min(w * 64 + lane, last_page), lds + uint32_t(w & 1) * 256);
+    window = w;
+  }
+  // 4 bytes per lane from global memory into LDS (lane l at lds + 4 l)
+  static __device__ __forceinline__ void lds_load4(const void* src, uint32_t lds) {
+    uint32_t saved;
+    asm volatile(
+        "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\tglobal_load_lds_dword %1, off\n\t"
+        "s_mov_b32 m0, %0"
+        : "=&s"(saved)
+        : "v"(src), "s"(__builtin_amdgcn_readfirstlane(lds))
+        : "memory");
+  }
+  // The windows of keys [key0, ..): call with the first key of the segment,
+  // and wait for the loads before get().
+  __device__ __forceinline__ void start(int key0, int last) {
+    const int w = (key0 >> psl) >> 6;
+    load(w, last >> psl);
+    load(w + 1, last >> psl);
+  }
+  // before the keys of page index j are asked for: the window behind j's is in flight
+  __device__ __forceinline__ void ahead(int j, int last) {
+    if ((j >> 6) == window) load(window + 1, last >> psl);
+  }
+  __device__ __forceinline__ int64_t get(int j) const {
+    const unsigned p = __builtin_amdgcn_readfirstlane(slots[((j >> 6) & 1) * 64 + (j & 63)]);
+    return p < unsigned(n_pages) ? p : 0;
+  }
+};
+
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+__device__ __forceinline__ bool odd_bf16x2(uint32_t w) {   // one of two is not finite
+  return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
+}
+
+// Rows of 1 KiB loads of a V tile from 16-byte place x on: are all finite / made 0 where not
+__device__ __forceinline__ bool odd16(const char* p) {
+  const uint4 x = ld16(p);
+  return odd_bf16x2(x.x) || odd_bf16x2(x.y) || odd_bf16x2(x.z) || odd_bf16x2(x.w);
+}
+__device__ __forceinline__ void clear_odd16(char* p) {
+  const uint4 x = ld16(p);
+  uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if ((w[e] & 0x7f80u) == 0x7f80u) w[e] &= 0xffff0000u;
+    if ((w[e] & 0x7f800000u) == 0x7f800000u) w[e] &= 0xffffu;
+  }
+  st16(p, make_uint4(w[0], w[1], w[2], w[3]));
+}
+
+// Adds what the elements of V row `key` that are not finite give to the
+// queries that see it (p: this lane's query's probability of the key).
+template <int D>
+__device__ __forceinline__ void add_odd_row(const char* sV, int key, float p, bool sees,
+                                            f32x16 (&oacc)[D / 32]) {
+  const int g = (threadIdx.x & 63) >> 5;
+  const char* row = sV + key * (D * 2) + g * 8;
+  const int swz = kv_swz<D>(key) << 4;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int q4 = 0; q4 < 4; ++q4) {   // dims db * 32 + q4 * 8 + g * 4 .. + 4
+      const uint2 x = *reinterpret_cast<const uint2*>(row + (((db * 4 + q4) << 4) ^ swz));
+      const uint32_t w[4] = {x.x & 0xffffu, x.x >> 16, x.y & 0xffffu, x.y >> 16};
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if ((w[e] & 0x7f80u) == 0x7f80u && sees)
+          oacc[db][q4 * 4 + e] += p * bf16_to_f32(uint16_t(w[e]));
+      asm volatile("" ::: "memory");   // (a row at a time: this path is rare, registers are not)
+    }
+}
+
+// Pair m of a tile: its row of q and its head
+struct Pair {
+  int i, h;
+  int64_t row;
+  __device__ __forceinline__ Pair(const TreeArgs& a, const Tile& t, int hk, int m) {
+    i = m / a.G;
+    h = hk * a.G + m - i * a.G;
+    row = int64_t(t.r0) + i;
+  }
+};
+
+// --------------------------------------------------------------------------
+// few pairs: NW waves, each with two K and two V tiles of 32 keys
+// --------------------------------------------------------------------------
 template <int D, int NW>
-__global__ __launch_bounds__(NW * 64) void tree_attn_kernel(TreeArgs a) {
+__global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
   constexpr int R = 32, BLOCK = NW * 64;
   constexpr int KS = D / 16, DB = D / 32;
   constexpr int TB = 32 * D * 2;             // bytes of a tile
   constexpr int NI = TB / 1024;              // 1 KiB loads of a tile
   constexpr int LR = 512 / D;                // rows of a load
-  constexpr int PG = 128;                    // page ids held per wave
   constexpr int OS = D + 4;                  // floats of a row of O where the waves meet
   static_assert(R * OS * 4 <= 4 * TB, "a wave's O fits its tiles");
   __shared__ __align__(1024) char buf[NW][4 * TB];   // K, K, V, V
+  __shared__ __align__(16) int pg[NW][128];
   __shared__ TreeShared sh;
-  __shared__ int pg[NW][PG];
   __shared__ float sm[NW][R], sl[NW][R];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int c = lane & 31, g = lane >> 5;
-  const int hk = blockIdx.x % a.Hkv;
-
-  load_sizes(a, sh);
-  const int run = run_length<R, BLOCK>(a, sh);
-  find_run<R, BLOCK>(a, sh, run, blockIdx.x / a.Hkv, false);
-  const int place = sh.found[0];
-  if (place < 0) return;
-  const int ri = sh.found[1], runs = sh.found[2];
-  const Tile t = tile_of<R>(a, sh, place);
-  const int id = a.ids[t.b];
-  const int64_t row0 = t.r0;
-
-  // Q^T as the B operand: lane holds pair c, dims ks*16 + g*8 .. + 8
-  const bool qok = c < t.rows;
-  const int m = t.m0 + (qok ? c : 0);
-  const int qi = m / a.G;
-  const int64_t qrow = row0 + qi;
-  const int64_t qat = (qrow * a.Hq + hk * a.G + (m - qi * a.G)) * D;
-  bf16x8 qf[KS];
-#pragma unroll
-  for (int ks = 0; ks < KS; ++ks)
-    qf[ks] = as_bf16x8(qok ? ld16(a.q + qat + ks * 16 + g * 8) : make_uint4(0, 0, 0, 0));
-
-  f32x16 oacc[DB];
-#pragma unroll
-  for (int db = 0; db < DB; ++db)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) oacc[db][r] = 0.f;
-  float m_run = -INFINITY, l_run = 0.f;
-
-  // this run's keys; wave w takes 32-key tiles w, w + NW, ...
-  const int units = max(1, (t.kmax + kUnit - 1) / kUnit);
-  const int k_begin = int(int64_t(ri) * run) * kUnit;
-  const int k_end = int(min(int64_t(t.kmax), int64_t(min(units, (ri + 1) * run)) * kUnit));
-  const int nt = max(0, (k_end - k_begin + 31) / 32);
-  const int mine = nt > wave ? (nt - wave + NW - 1) / NW : 0;
-  auto key_of = [&](int x) { return k_begin + (wave + x * NW) * 32; };
-
-  // page ids of the keys ahead: entries [pg0, pg0 + PG) of the sequence's table
-  const int last = t.kmax - 1;
+  Deal<R, BLOCK> deal(a, sh);
+  const int run = run_of_block(a.groups);
+  const int64_t begin = run * deal.per;
+  const int64_t end = min(begin + deal.per, deal.units * a.Hkv);
   const int ps = 1 << a.psl;
-  int pg0 = -PG;
-  auto fill_pages = [&](int first) {
-    pg0 = first;
-    for (int j = lane; j < PG; j += 64) {
-      int p = 0;
-      if (first + j <= last >> a.psl) {
-        p = a.table[int64_t(id) * a.max_pages + first + j];
-        p = unsigned(p) < unsigned(a.n_pages) ? p : 0;
-      }
-      pg[wave][j] = p;
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  };
-  const int64_t page_bytes = int64_t(a.Hkv) * ps * D * 2;
-  const char* kb = reinterpret_cast<const char*>(a.k) + int64_t(hk) * ps * D * 2;
-  const char* vb = reinterpret_cast<const char*>(a.v) + int64_t(hk) * ps * D * 2;
   const int lrow = lane / (D / 8), lpos = lane % (D / 8);
   const uint32_t lds0 = lds_addr(&buf[wave][0]);
-  // Tile x of this wave into buffer x & 1.  Keys past the last read the last
-  // (a load's rows lie in one page; what is past it is masked).
-  auto issue = [&](int x) {
-    const int key0 = key_of(x);
-    const int p_lo = min(key0, last) >> a.psl, p_hi = min(key0 + 31, last) >> a.psl;
-    if (p_lo < pg0 || p_hi >= pg0 + PG) fill_pages(p_lo);
-    const uint32_t kl = lds0 + uint32_t(x & 1) * TB;
-#pragma unroll
-    for (int j = 0; j < NI; ++j) {
-      const int key = min(key0 + j * LR, last);
-      const int64_t page = __builtin_amdgcn_readfirstlane(pg[wave][(key >> a.psl) - pg0]);
-      const int r = j * LR + lrow;
-      const uint32_t off = uint32_t(min(key0 + r, last) & (ps - 1)) * (D * 2) +
-                           uint32_t((lpos ^ kv_swz<D>(r)) << 4);
-      lds_load16s(uniform_ptr(kb + page * page_bytes), off, kl + j * 1024);
-      lds_load16s(uniform_ptr(vb + page * page_bytes), off, kl + 2 * TB + j * 1024);
-    }
-  };
 
-  if (mine > 0) issue(0);
-  if (mine > 1) issue(1);
-  const int clear = a.tree ? t.c : t.c + t.m0 / a.G + 1;   // keys every row of the tile sees
-  for (int x = 0; x < mine; ++x) {
-    // the tile has landed (the next one's loads may be in flight)
-    if (x + 1 < mine)
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NI) : "memory");
-    else
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    const char* sK = &buf[wave][(x & 1) * TB];
-    const char* sV = sK + 2 * TB;
-    f32x16 sc = {};
+  for (int64_t p = begin; p < end;) {
+    const int hk = uniform(int(p / deal.units));
+    int place, unit;
+    deal.find(p - hk * deal.units, place, unit);
+    const Tile t = uniform(tile_of<R>(a, sh, place));
+    const int units = t.units();
+    const int n_units = int(min(int64_t(units - unit), end - p));
+
+    // Q^T as the B operand: lane holds pair c, dims ks*16 + g*8 .. + 8
+    const bool qok = c < t.rows;
+    const Pair mine(a, t, hk, t.m0 + (qok ? c : 0));
+    bf16x8 qf[KS];
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) sc = mfma32(ld_row_swz<D>(sK, c, ks * 2 + g), qf[ks], sc);
-    const int key0 = key_of(x);
-    uint32_t see = ~0u;
-    const bool masked = key0 + 32 > min(clear, k_end);   // wave-uniform
-    if (masked) {
-      const int n = k_end - key0;
-      see = seen32(a, t, qrow, qi, key0) & (n >= 32 ? ~0u : (1u << n) - 1u);
+    for (int ks = 0; ks < KS; ++ks)
+      qf[ks] = as_bf16x8(qok ? ld16(a.q + (mine.row * a.Hq + mine.h) * D + ks * 16 + g * 8)
+                             : make_uint4(0, 0, 0, 0));
+    f32x16 oacc[DB];
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        sc[r] = (see >> ((r >> 2) * 8 + g * 4 + (r & 3))) & 1u ? sc[r] : -INFINITY;
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) oacc[db][r] = 0.f;
+    float m_run = -INFINITY, l_run = 0.f;
+
+    // this segment's keys; wave w takes 32-key tiles w, w + NW, ...
+    const int k_begin = unit * kUnit;
+    const int k_end = int(min(int64_t(t.kmax), int64_t(unit + n_units) * kUnit));
+    const int nt = k_end > k_begin ? (k_end - k_begin + 31) / 32 : 0;
+    const int todo = nt > wave ? (nt - wave + NW - 1) / NW : 0;
+    auto key_of = [&](int x) { return k_begin + (wave + x * NW) * 32; };
+    const int last = t.kmax - 1;
+    const int64_t page_bytes = int64_t(a.Hkv) * ps * D * 2;
+    const char* kb = reinterpret_cast<const char*>(a.k) + int64_t(hk) * ps * D * 2;
+    const char* vb = reinterpret_cast<const char*>(a.v) + int64_t(hk) * ps * D * 2;
+    PageRing pages{nullptr, lds_addr(&pg[wave][0]), &pg[wave][0], 0, a.n_pages, a.psl};
+    if (todo > 0) {
+      pages.row = a.table + int64_t(a.ids[t.b]) * a.max_pages;
+      pages.start(key_of(0), last);
+      wait_loads<0>();
     }
-    float mx = sc[0];
-#pragma unroll
-    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sc[r]);
-    mx = max_halves(mx) * a.scale_log2;
-    if (__any(mx > m_run)) {
-      const float m_new = fmaxf(m_run, mx);
-      const float alpha = m_run == -INFINITY ? 0.f : fast_exp2(m_run - m_new);
-      m_run = m_new;
-      l_run *= alpha;
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) oacc[db][r] *= alpha;
-    }
-    const float mu = m_run == -INFINITY ? 0.f : m_run;
-    // P in bf16 for the product (its sum is taken before the rounding): half
-    // an ulp of each, 2^-8 relative, averaged over the row
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      sc[r] = fast_exp2(fmaf(sc[r], a.scale_log2, -mu));
-      l_run += sc[r];
-    }
-    if (masked) {
-      // A value that is not finite in a row that some query does not see
-      // would reach it as 0 * inf: such elements are taken out of the tile
-      // and added, query by query, where they are seen.
-      bool odd = false;
+    // Tile x of this wave into buffer x & 1.  Keys past the last read the last
+    // (a load's rows lie in one page; what is past it is masked).
+    auto issue = [&](int x) {
+      const int key0 = key_of(x);
+      pages.ahead(key0 >> a.psl, last);
+      const uint32_t kl = lds0 + uint32_t(x & 1) * TB;
 #pragma unroll
       for (int j = 0; j < NI; ++j) {
-        const uint4 x4 = ld16(sV + j * 1024 + lane * 16);
-        const uint32_t w[4] = {x4.x, x4.y, x4.z, x4.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          odd |= (w[e] & 0x7f80u) == 0x7f80u || (w[e] & 0x7f800000u) == 0x7f800000u;
+        const int64_t page = pages.get(min(key0 + j * LR, last) >> a.psl);
+        const int r = j * LR + lrow;
+        const uint32_t off = uint32_t(min(key0 + r, last) & (ps - 1)) * (D * 2) +
+                             uint32_t((lpos ^ kv_swz<D>(r)) << 4);
+        lds_load16s(uniform_ptr(kb + page * page_bytes), off, kl + j * 1024);
+        lds_load16s(uniform_ptr(vb + page * page_bytes), off, kl + 2 * TB + j * 1024);
       }
-      if (__any(odd)) {
-        for (int key = 0; key < 32; ++key) {
-          const int rr = (key >> 3) * 4 + (key & 3), hh = (key >> 2) & 1;
-          float p = 0.f;
+    };
+    if (todo > 0) issue(0);
+    if (todo > 1) issue(1);
+    const int clear = a.tree ? t.c : t.c + t.m0 / a.G + 1;   // keys every row of the tile sees
+    for (int x = 0; x < todo; ++x) {
+      // the tile has landed (the next one's loads may be in flight)
+      if (x + 1 < todo)
+        wait_loads<2 * NI>();
+      else
+        wait_loads<0>();
+      const char* sK = &buf[wave][(x & 1) * TB];
+      char* sV = &buf[wave][(x & 1) * TB + 2 * TB];
+      f32x16 sc = {};
 #pragma unroll
-          for (int r = 0; r < 16; ++r) p = r == rr ? sc[r] : p;
-          p = __shfl(p, c + 32 * hh);
-          if (!__any((see >> key) & 1u)) continue;
+      for (int ks = 0; ks < KS; ++ks) sc = mfma32(ld_row_swz<D>(sK, c, ks * 2 + g), qf[ks], sc);
+      const int key0 = key_of(x);
+      uint32_t see = ~0u;
+      const bool masked = key0 + 32 > min(clear, k_end);   // wave-uniform
+      if (masked) {
+        const int n = k_end - key0;
+        see = seen32(a, t, mine.row, mine.i, key0) & (n >= 32 ? ~0u : (1u << n) - 1u);
 #pragma unroll
-          for (int db = 0; db < DB; ++db)
+        for (int r = 0; r < 16; ++r)
+          sc[r] = (see >> ((r >> 2) * 8 + g * 4 + (r & 3))) & 1u ? sc[r] : -INFINITY;
+      }
+      float mx = sc[0];
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const int dim = db * 32 + (r >> 2) * 8 + g * 4 + (r & 3);
-              const u16 b = *reinterpret_cast<const u16*>(
-                  sV + key * (D * 2) + (((dim >> 3) ^ kv_swz<D>(key)) << 4) + (dim & 7) * 2);
-              if ((b & 0x7f80u) == 0x7f80u && ((see >> key) & 1u))
-                oacc[db][r] += p * bf16_to_f32(b);
-            }
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        char* wV = const_cast<char*>(sV);
+      for (int r = 1; r < 16; ++r) mx = fmaxf(mx, sc[r]);
+      mx = max_halves(mx) * a.scale_log2;
+      if (__any(mx > m_run)) {
+        const float m_new = fmaxf(m_run, mx);
+        const float alpha = m_run == -INFINITY ? 0.f : fast_exp2(m_run - m_new);
+        m_run = m_new;
+        l_run *= alpha;
 #pragma unroll
-        for (int j = 0; j < NI; ++j) {
-          uint4 x4 = ld16(wV + j * 1024 + lane * 16);
-          uint32_t w[4] = {x4.x, x4.y, x4.z, x4.w};
+        for (int db = 0; db < DB; ++db)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if ((w[e] & 0x7f80u) == 0x7f80u) w[e] &= 0xffff0000u;
-            if ((w[e] & 0x7f800000u) == 0x7f800000u) w[e] &= 0xffffu;
+          for (int r = 0; r < 16; ++r) oacc[db][r] *= alpha;
+      }
+      const float mu = m_run == -INFINITY ? 0.f : m_run;
+      // P in bf16 for the product (its sum is taken before the rounding): half
+      // an ulp of each, 2^-8 relative, averaged over the row
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        sc[r] = fast_exp2(fmaf(sc[r], a.scale_log2, -mu));
+        l_run += sc[r];
+      }
+      if (masked) {
+        // A value that is not finite in a row that some query does not see
+        // would reach it as 0 * inf: such elements are taken out of the tile
+        // and added, query by query, where they are seen.
+        bool odd = false;
+#pragma unroll
+        for (int j = 0; j < NI; ++j) odd |= odd16(sV + j * 1024 + lane * 16);
+        if (__any(odd)) {
+#pragma nounroll
+          for (int key = 0; key < 32; ++key) {
+            const int rr = (key >> 3) * 4 + (key & 3), hh = (key >> 2) & 1;
+            float pk = 0.f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) pk = r == rr ? sc[r] : pk;
+            pk = __shfl(pk, c + 32 * hh);
+            add_odd_row<D>(sV, key, pk, (see >> key) & 1u, oacc);
           }
-          st16(wV + j * 1024 + lane * 16, make_uint4(w[0], w[1], w[2], w[3]));
+          wait_lds();
+#pragma unroll
+          for (int j = 0; j < NI; ++j) clear_odd16(sV + j * 1024 + lane * 16);
+          wait_lds();
         }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      }
+      const bf16x8 pf[2] = {to_operand(sc, 0), to_operand(sc, 8)};
+#pragma unroll
+      for (int st = 0; st < 2 * DB; ++st)
+        oacc[st % DB] = mfma32(ld_tr_swz<D>(sV, (st / DB) * 16, (st % DB) * 32), pf[st / DB],
+                               oacc[st % DB]);
+      if (x + 2 < todo) {
+        wait_lds();   // the buffer's reads are done
+        issue(x + 2);
       }
     }
-    const bf16x8 pf[2] = {to_operand(sc, 0), to_operand(sc, 8)};
-#pragma unroll
-    for (int st = 0; st < 2 * DB; ++st)
-      oacc[st % DB] = mfma32(ld_tr_swz<D>(sV, (st / DB) * 16, (st % DB) * 32), pf[st / DB],
-                             oacc[st % DB]);
-    if (x + 2 < mine) {
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the buffer's reads are done
-      issue(x + 2);
-    }
-  }
-  l_run += __shfl_xor(l_run, 32);
+    l_run += __shfl_xor(l_run, 32);
 
-  // the waves' results meet: each scales its own to the common maximum
-  if (g == 0) {
-    sm[wave][c] = m_run;
-    sl[wave][c] = l_run;
-  }
-  __syncthreads();
-  float M = sm[0][c];
-#pragma unroll
-  for (int w = 1; w < NW; ++w) M = fmaxf(M, sm[w][c]);
-  const float f = weight(m_run, M);
-  float* so = reinterpret_cast<float*>(&buf[wave][0]);
-#pragma unroll
-  for (int db = 0; db < DB; ++db)
-#pragma unroll
-    for (int q4 = 0; q4 < 4; ++q4) {
-      float4 x4;
-      x4.x = oacc[db][q4 * 4 + 0] * f;
-      x4.y = oacc[db][q4 * 4 + 1] * f;
-      x4.z = oacc[db][q4 * 4 + 2] * f;
-      x4.w = oacc[db][q4 * 4 + 3] * f;
-      *reinterpret_cast<float4*>(so + c * OS + db * 32 + q4 * 8 + g * 4) = x4;
+    // the waves' results meet: each scales its own to the common maximum
+    if (g == 0) {
+      sm[wave][c] = m_run;
+      sl[wave][c] = l_run;
     }
-  __syncthreads();
-  for (int x = tid; x < t.rows * (D / 8); x += BLOCK) {
-    const int r = x / (D / 8), d0 = (x % (D / 8)) * 8;
-    float Mr = sm[0][r], l = 0.f;
+    __syncthreads();
+    float M = sm[0][c];
 #pragma unroll
-    for (int w = 1; w < NW; ++w) Mr = fmaxf(Mr, sm[w][r]);
+    for (int w = 1; w < NW; ++w) M = fmaxf(M, sm[w][c]);
+    const float f = weight(m_run, M);
+    float* so = reinterpret_cast<float*>(&buf[wave][0]);
 #pragma unroll
-    for (int w = 0; w < NW; ++w) l += sl[w][r] * weight(sm[w][r], Mr);
-    float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int db = 0; db < DB; ++db)
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      const float* p = reinterpret_cast<const float*>(&buf[w][0]) + r * OS + d0;
+      for (int q4 = 0; q4 < 4; ++q4)
+        *reinterpret_cast<float4*>(so + c * OS + db * 32 + q4 * 8 + g * 4) =
+            make_float4(oacc[db][q4 * 4 + 0] * f, oacc[db][q4 * 4 + 1] * f,
+                        oacc[db][q4 * 4 + 2] * f, oacc[db][q4 * 4 + 3] * f);
+    __syncthreads();
+    const bool whole = n_units == units;
+    const int64_t slot = 2 * int64_t(run) + (p != begin);
+    for (int x = tid; x < t.rows * (D / 8); x += BLOCK) {
+      const int r = x / (D / 8), d0 = (x % (D / 8)) * 8;
+      float Mr = sm[0][r], l = 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] += p[e];
-    }
-    if (runs == 1) {
-      const int mm = t.m0 + r, i = mm / a.G, h = hk * a.G + mm - i * a.G;
-      const float inv = l == 0.f ? 0.f : 1.f / l;   // l is 0 where no key was seen
+      for (int w = 1; w < NW; ++w) Mr = fmaxf(Mr, sm[w][r]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] *= inv;
-      store_v<8>(a.o + ((row0 + i) * a.Hq + h) * D + d0, y);
-      if (d0 == 0)
-        a.lse[int64_t(h) * a.N + row0 + i] =
-            l == 0.f ? -INFINITY : (Mr + __log2f(l)) * 0.69314718055994531f;
-    } else {
-      float* p = a.part_o + (int64_t(blockIdx.x) * R + r) * D + d0;
-      *reinterpret_cast<float4*>(p) = make_float4(y[0], y[1], y[2], y[3]);
-      *reinterpret_cast<float4*>(p + 4) = make_float4(y[4], y[5], y[6], y[7]);
-      if (d0 == 0) {
-        a.part_ml[(int64_t(blockIdx.x) * R + r) * 2] = Mr;
-        a.part_ml[(int64_t(blockIdx.x) * R + r) * 2 + 1] = l;
+      for (int w = 0; w < NW; ++w) l += sl[w][r] * weight(sm[w][r], Mr);
+      float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        const float* q = reinterpret_cast<const float*>(&buf[w][0]) + r * OS + d0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] += q[e];
+      }
+      if (whole) {
+        const Pair pr(a, t, hk, t.m0 + r);
+        const float inv = l == 0.f ? 0.f : 1.f / l;   // l is 0 where no key was seen
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] *= inv;
+        store_v<8>(a.o + (pr.row * a.Hq + pr.h) * D + d0, y);
+        if (d0 == 0)
+          a.lse[int64_t(pr.h) * a.N + pr.row] =
+              l == 0.f ? -INFINITY : (Mr + __log2f(l)) * 0.69314718055994531f;
+      } else {
+        float* q = a.part_o + (slot * R + r) * D + d0;
+        *reinterpret_cast<float4*>(q) = make_float4(y[0], y[1], y[2], y[3]);
+        *reinterpret_cast<float4*>(q + 4) = make_float4(y[4], y[5], y[6], y[7]);
+        if (d0 == 0) {
+          a.part_ml[(slot * R + r) * 2] = Mr;
+          a.part_ml[(slot * R + r) * 2 + 1] = l;
+        }
       }
     }
+    __syncthreads();
+    p += n_units;
   }
 }
 
-// Joins the runs of a tile, in their order: block (tile place, KV head, rows
-// rg * RG ..), a thread to 8 elements of a row.
-template <int D, int R>
-__global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a) {
-  constexpr int RG = 256 / (D / 8);   // rows of a block
-  constexpr int NG = (R + RG - 1) / RG;
+// --------------------------------------------------------------------------
+// many pairs: four waves of 32 pairs on shared 64-key tiles
+// --------------------------------------------------------------------------
+template <int D>
+__global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
+  constexpr int R = 128, BK = 64, BLOCK = 256;
+  constexpr int KS = D / 16, DB = D / 32;
+  constexpr int TB = BK * D * 2;             // bytes of a tile
+  constexpr int NL = TB / 4096;              // loads of a thread per tile
+  constexpr int LR = 512 / D;                // rows of a wave's load
+  __shared__ __align__(1024) char sKb[2][TB];
+  __shared__ __align__(1024) char sVb[2][TB];
+  __shared__ __align__(16) int pg[4][128];
   __shared__ TreeShared sh;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int c = lane & 31, g = lane >> 5;
+  Deal<R, BLOCK> deal(a, sh);
+  const int run = run_of_block(a.groups);
+  const int64_t begin = run * deal.per;
+  const int64_t end = min(begin + deal.per, deal.units * a.Hkv);
+  const int ps = 1 << a.psl;
+  const int lrow = lane / (D / 8), lpos = lane % (D / 8);
+
+  for (int64_t p = begin; p < end;) {
+    const int hk = uniform(int(p / deal.units));
+    int place, unit;
+    deal.find(p - hk * deal.units, place, unit);
+    const Tile t = uniform(tile_of<R>(a, sh, place));
+    const int units = t.units();
+    const int n = int(min(int64_t(units - unit), end - p));   // 64-key tiles of the segment
+
+    const int my = wave * 32 + c;
+    const bool qok = my < t.rows;
+    // this lane's pair, worked out again where it is needed rather than held
+    auto pair = [&]() {
+      int m = t.m0 + (my < t.rows ? my : 0);
+      asm volatile("" : "+v"(m));
+      return Pair(a, t, hk, m);
+    };
+    bf16x8 qf[KS];
+    {
+      const Pair mine = pair();
+      const u16* qp = a.q + (mine.row * a.Hq + mine.h) * D + g * 8;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+        qf[ks] = as_bf16x8(qok ? ld16(qp + ks * 16) : make_uint4(0, 0, 0, 0));
+    }
+    f32x16 oacc[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) oacc[db][r] = 0.f;
+    float m_run = -INFINITY, l_run = 0.f;
+
+    const int key_base = unit * BK;
+    const int last = t.kmax - 1;
+    const int64_t page_bytes = int64_t(a.Hkv) * ps * D * 2;
+    const char* kb = reinterpret_cast<const char*>(a.k) + int64_t(hk) * ps * D * 2;
+    const char* vb = reinterpret_cast<const char*>(a.v) + int64_t(hk) * ps * D * 2;
+    PageRing pages{nullptr, lds_addr(&pg[wave][0]), &pg[wave][0], 0, a.n_pages, a.psl};
+    const bool keys = t.kmax > 0;   // block-uniform
+    if (keys) {
+      pages.row = a.table + int64_t(a.ids[t.b]) * a.max_pages;
+      pages.start(key_base, last);
+      wait_loads<0>();
+    }
+    // 64-key tile x of one tensor into the LDS tile at `lds`
+    auto issue = [&](const char* base, int x, uint32_t lds) {
+      const int key0 = key_base + x * BK;
+#pragma unroll
+      for (int j = 0; j < NL; ++j) {
+        const int r0 = (j * 4 + wave) * LR, r = r0 + lrow;
+        const int64_t page = pages.get(min(key0 + r0, last) >> a.psl);
+        const uint32_t off = uint32_t(min(key0 + r, last) & (ps - 1)) * (D * 2) +
+                             uint32_t((lpos ^ kv_swz<D>(r)) << 4);
+        lds_load16s(uniform_ptr(base + page * page_bytes), off,
+                    lds + uint32_t(j * 4 + wave) * 1024);
+      }
+    };
+    auto issue_k = [&](int x) { issue(kb, x, lds_addr(&sKb[x & 1][0])); };
+    // V runs a tile behind K, so it is V's tile that leaves a window for good
+    // (K needs the next one 15 tiles later at the earliest)
+    auto issue_v = [&](int x) {
+      pages.ahead((key_base + x * BK) >> a.psl, last);
+      issue(vb, x, lds_addr(&sVb[x & 1][0]));
+    };
+    auto kfrag = [&](int x, int j) {
+      return ld_row_swz<D>(&sKb[x & 1][0], (j & 1) * 32 + c, (j >> 1) * 2 + g);
+    };
+    const int clear = a.tree ? t.c : t.c + t.m0 / a.G + 1;   // keys every row of the tile sees
+    auto masked = [&](int x) { return key_base + x * BK + BK > min(clear, t.kmax); };
+    auto seen = [&](int x, int kb2) {   // of keys 32 kb2 .. + 32 of tile x
+      const int key0 = key_base + x * BK + kb2 * 32, m = t.kmax - key0;
+      const uint32_t in = m >= 32 ? ~0u : m <= 0 ? 0u : (1u << m) - 1u;
+      const Pair mine = pair();
+      return seen32(a, t, mine.row, mine.i, key0) & in;
+    };
+    f32x16 sc[2][2];   // scores of tile x in sc[x & 1]
+    auto mask_tile = [&](f32x16 (&s)[2], int x) {
+      if (!masked(x)) return;   // block-uniform
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const uint32_t w = seen(x, b) >> (g * 4);
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          s[b][r] = (w >> ((r >> 2) * 8 + (r & 3))) & 1u ? s[b][r] : -INFINITY;
+      }
+    };
+    auto tile_max = [&](const f32x16 (&s)[2]) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[b][r]);
+      return max_halves(mx) * a.scale_log2;
+    };
+    // As in the masked forward: probabilities are taken against the maximum of
+    // a tile that the row has scored before; only where they would pass 2^16,
+    // or a row has seen no key yet, is the tile's own maximum taken.
+    auto m_off = [&]() { return m_run == -INFINITY ? 0.f : m_run; };
+    auto pexp = [&](const f32x16 (&s)[2], int i, float mu) {
+      return fast_exp2(fmaf(s[i >> 4][i & 15], a.scale_log2, -mu));
+    };
+    auto pack8 = [](const float* q) {
+      return as_bf16x8(make_uint4(pack2(q[0], q[1]), pack2(q[2], q[3]), pack2(q[4], q[5]),
+                                  pack2(q[6], q[7])));
+    };
+    auto slow_tile = [&](const f32x16 (&s)[2], bf16x8 (&pf)[4], float& psum)
+                         __attribute__((always_inline)) {
+      const float m_tile = tile_max(s);
+      if (m_tile > m_run) {
+        const float alpha = m_run == -INFINITY ? 0.f : fast_exp2(m_run - m_tile);
+        m_run = m_tile;
+        l_run *= alpha;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) oacc[db][r] *= alpha;
+      }
+      const float mu = m_off();
+      psum = 0.f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        float q[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          q[u] = pexp(s, 8 * k + u, mu);
+          psum += q[u];
+        }
+        pf[k] = pack8(q);
+      }
+    };
+    // Values that are not finite in a masked tile (see the kernel for few
+    // pairs): added where they are seen, then made 0.
+    auto odd_values = [&](const f32x16 (&s)[2], int x) __attribute__((always_inline)) {
+      char* sV = &sVb[x & 1][0];
+      bool odd = false;
+#pragma unroll
+      for (int j = 0; j < NL; ++j) odd |= odd16(sV + (j * 4 + wave) * 1024 + lane * 16);
+      if (!__syncthreads_or(odd)) return;
+      const float mu = m_off();
+      const uint32_t see0 = seen(x, 0), see1 = seen(x, 1);
+#pragma nounroll
+      for (int key = 0; key < BK; ++key) {
+        const int kk = key & 31, rr = (kk >> 3) * 4 + (kk & 3), hh = (kk >> 2) & 1;
+        float sk = 0.f;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) sk = b * 16 + r == (key >> 5) * 16 + rr ? s[b][r] : sk;
+        sk = __shfl(sk, c + 32 * hh);
+        add_odd_row<D>(sV, key, fast_exp2(fmaf(sk, a.scale_log2, -mu)),
+                       ((key < 32 ? see0 : see1) >> kk) & 1u, oacc);
+      }
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < NL; ++j) clear_odd16(sV + (j * 4 + wave) * 1024 + lane * 16);
+      __syncthreads();
+    };
+
+    bf16x8 pf[4];
+    float psum_a = 0.f;
+    if (keys) {
+      issue_k(0);
+      if (n > 1) issue_k(1);
+      issue_v(0);
+      wait_loads<0>();
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < 2 * KS; ++j)
+        sc[0][j & 1] = mfma32(kfrag(0, j), qf[j >> 1], j < 2 ? f32x16{} : sc[0][j & 1]);
+      mask_tile(sc[0], 0);
+      m_run = tile_max(sc[0]);
+      const float mu = m_off();
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        float q[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          q[u] = pexp(sc[0], 8 * k + u, mu);
+          psum_a += q[u];
+        }
+        pf[k] = pack8(q);
+      }
+    }
+    // One step: tile x (scores in set P, its first two operands in pf) and the
+    // scores of tile x + 1.  On the last tile the score MFMAs run on stale
+    // LDS and their results are dropped.
+    auto step = [&](auto par, int x) __attribute__((always_inline)) {
+      constexpr int P = decltype(par)::value;
+      f32x16 (&cur)[2] = sc[P];
+      f32x16 (&nxt)[2] = sc[P ^ 1];
+      const bool next = x + 1 < n;   // block-uniform
+      // K of tile x + 1 and V of tile x have landed, every wave is done with
+      // K of tile x and V of tile x - 1
+      wait_loads<0>();
+      __syncthreads();
+      if (x + 2 < n) issue_k(x + 2);
+      if (next) issue_v(x + 1);
+      const float mu = m_off();
+      float psum = psum_a;
+      {
+        bf16x8 kr[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) kr[j] = kfrag(x + 1, j);
+        float q[16];
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < 2 * KS; ++j) {
+          nxt[j & 1] = mfma32(kr[j & 3], qf[j >> 1], j < 2 ? f32x16{} : nxt[j & 1]);
+          if (j + 4 < 2 * KS) kr[j & 3] = kfrag(x + 1, j + 4);
+          constexpr int NS = 2 * KS;
+          const int i0 = 16 * j / NS, i1 = 16 * (j + 1) / NS;
+#pragma unroll
+          for (int i = i0; i < i1; ++i) {
+            q[i] = pexp(cur, 16 + i, mu);
+            psum += q[i];
+          }
+          if (i1 / 8 != i0 / 8) {
+            const int k = i1 / 8 - 1;
+            pf[2 + k] = pack8(q + 8 * k);
+            asm volatile("" : "+v"(pf[2 + k]));
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      if (__any(!(psum <= 65536.f) || (qok && m_run == -INFINITY))) slow_tile(cur, pf, psum);
+      l_run += psum;
+      if (masked(x)) odd_values(cur, x);
+      if (next) mask_tile(nxt, x + 1);
+      {
+        const float mu1 = m_off();
+        const char* sV = &sVb[x & 1][0];
+        auto vfrag = [&](int st) { return ld_tr_swz<D>(sV, (st / DB) * 16, (st % DB) * 32); };
+        bf16x8 vr[4];
+#pragma unroll
+        for (int st = 0; st < 4; ++st) vr[st] = vfrag(st);
+        float q[16];
+        psum_a = 0.f;
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int st = 0; st < 4 * DB; ++st) {
+          oacc[st % DB] = mfma32(vr[st & 3], pf[st / DB], oacc[st % DB]);
+          if (st + 4 < 4 * DB) vr[st & 3] = vfrag(st + 4);
+          constexpr int NS = 4 * DB;
+          const int i0 = 16 * st / NS, i1 = 16 * (st + 1) / NS;
+#pragma unroll
+          for (int i = i0; i < i1; ++i) {
+            q[i] = pexp(nxt, i, mu1);
+            psum_a += q[i];
+          }
+          if (i1 / 8 != i0 / 8) {
+            const int k = i1 / 8 - 1;
+            pf[k] = pack8(q + 8 * k);
+            asm volatile("" : "+v"(pf[k]));
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        asm volatile("" : "+v"(psum_a));
+      }
+    };
+    if (keys) {
+      using p0 = std::integral_constant<int, 0>;
+      using p1 = std::integral_constant<int, 1>;
+      for (int x = 0; x < n; x += 2) {
+        step(p0{}, x);
+        if (x + 1 < n) step(p1{}, x + 1);
+      }
+    }
+    const float l = l_run + __shfl_xor(l_run, 32);
+    if (qok) {
+      const Pair mine = pair();
+      if (n == units) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;   // l is 0 where no key was seen
+        u16* op = a.o + (mine.row * a.Hq + mine.h) * D;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int q4 = 0; q4 < 4; ++q4)
+            *reinterpret_cast<uint2*>(op + db * 32 + q4 * 8 + g * 4) =
+                make_uint2(pack2(oacc[db][q4 * 4 + 0] * inv, oacc[db][q4 * 4 + 1] * inv),
+                           pack2(oacc[db][q4 * 4 + 2] * inv, oacc[db][q4 * 4 + 3] * inv));
+        if (g == 0)
+          a.lse[int64_t(mine.h) * a.N + mine.row] =
+              l == 0.f ? -INFINITY : (m_run + __log2f(l)) * 0.69314718055994531f;
+      } else {
+        const int64_t s = (2 * int64_t(run) + (p != begin)) * R + my;
+        float* op = a.part_o + s * D;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int q4 = 0; q4 < 4; ++q4)
+            *reinterpret_cast<float4*>(op + db * 32 + q4 * 8 + g * 4) =
+                make_float4(oacc[db][q4 * 4 + 0], oacc[db][q4 * 4 + 1], oacc[db][q4 * 4 + 2],
+                            oacc[db][q4 * 4 + 3]);
+        if (g == 0) {
+          a.part_ml[s * 2] = m_run;
+          a.part_ml[s * 2 + 1] = l;
+        }
+      }
+    }
+    __syncthreads();   // the tiles are read before the next segment's loads
+    p += n;
+  }
+}
+
+// --------------------------------------------------------------------------
+// Joins the segments of a tile, in their order: block (tile place, KV head,
+// RG pairs), JG groups of D / 4 threads to a pair, each for every JG-th segment.
+// --------------------------------------------------------------------------
+template <int D, int R, int JG>
+__global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a) {
+  constexpr int TD = D / 4, RG = 256 / (TD * JG), NG = R / RG;
+  __shared__ float so[JG][RG][D], sml[JG][RG][2];
   int x = blockIdx.x;
   const int rg = x % NG;
   x /= NG;
   const int hk = x % a.Hkv, place = x / a.Hkv;
-  load_sizes(a, sh);
-  const Tile t = tile_of<R>(a, sh, place);
-  const int r = rg * RG + threadIdx.x / (D / 8), d0 = (threadIdx.x % (D / 8)) * 8;
-  if (rg * RG >= t.rows) return;   // block-uniform
-  const int run = run_length<R, 256>(a, sh);
-  find_run<R, 256>(a, sh, run, place, true);
-  const int first = sh.found[1], runs = sh.found[2];
-  if (runs <= 1 || r >= t.rows) return;
-  float M = -INFINITY;
-  for (int j = 0; j < runs; ++j)
-    M = fmaxf(M, a.part_ml[((int64_t(first + j) * a.Hkv + hk) * R + r) * 2]);
-  float l = 0.f, y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int j = 0; j < runs; ++j) {
-    const int64_t s = (int64_t(first + j) * a.Hkv + hk) * R + r;
-    const float mj = a.part_ml[2 * s], lj = a.part_ml[2 * s + 1];
-    const float f = weight(mj, M);
-    l += lj * f;
-    const float4 u = *reinterpret_cast<const float4*>(a.part_o + s * D + d0);
-    const float4 v = *reinterpret_cast<const float4*>(a.part_o + s * D + d0 + 4);
-    y[0] += u.x * f, y[1] += u.y * f, y[2] += u.z * f, y[3] += u.w * f;
-    y[4] += v.x * f, y[5] += v.y * f, y[6] += v.z * f, y[7] += v.w * f;
+  const int64_t units = a.plan[0], first = a.plan[1 + place];
+  const int64_t next = place + 1 < a.tiles ? a.plan[2 + place] : units;
+  const int64_t per = max(int64_t(1), (units * a.Hkv + a.groups - 1) / a.groups);
+  const int64_t p0 = hk * units + first, p1 = hk * units + next;
+  // the runs that hold units [p0, p1)
+  const int64_t g0 = p0 / per, g1 = p1 > p0 ? (p1 - 1) / per : g0;
+  if (g0 == g1) return;   // written whole (or no tile)
+  const int d0 = (threadIdx.x % TD) * 4, rr = threadIdx.x / TD % RG, jg = threadIdx.x / (TD * RG);
+  const int r = rg * RG + rr;
+  // the entry, from its place
+  int lo = 0, hi = a.B;
+  auto at = [&](int b) { return min(max(a.ptr[b], 0), a.N); };
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (first_place<R>(at(mid), mid, a.G) <= place) lo = mid; else hi = mid;
   }
-  const int mm = t.m0 + r, i = mm / a.G, h = hk * a.G + mm - i * a.G;
-  const int64_t row = int64_t(t.r0) + i;
+  Tile t;
+  t.r0 = at(lo);
+  t.m0 = (place - first_place<R>(t.r0, lo, a.G)) * R;
+  t.rows = min(R, (at(lo + 1) - t.r0) * a.G - t.m0);
+  if (rg * RG >= t.rows) return;   // block-uniform
+  auto slot = [&](int64_t run) { return (2 * run + (run * per < p0)) * R + r; };
+  float M = -INFINITY, l = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
+  if (r < t.rows) {
+    for (int64_t j = g0 + jg; j <= g1; j += JG) M = fmaxf(M, a.part_ml[2 * slot(j)]);
+#pragma unroll 4
+    for (int64_t j = g0 + jg; j <= g1; j += JG) {
+      const int64_t s = slot(j);
+      const float f = weight(a.part_ml[2 * s], M);
+      l += a.part_ml[2 * s + 1] * f;
+      const float4 u = *reinterpret_cast<const float4*>(a.part_o + s * D + d0);
+      y[0] += u.x * f, y[1] += u.y * f, y[2] += u.z * f, y[3] += u.w * f;
+    }
+  }
+  if (JG > 1) {
+    *reinterpret_cast<float4*>(&so[jg][rr][d0]) = make_float4(y[0], y[1], y[2], y[3]);
+    if (d0 == 0) {
+      sml[jg][rr][0] = M;
+      sml[jg][rr][1] = l;
+    }
+    __syncthreads();
+    if (jg != 0) return;
+#pragma unroll
+    for (int j = 1; j < JG; ++j) M = fmaxf(M, sml[j][rr][0]);
+    l = 0.f;
+    y[0] = y[1] = y[2] = y[3] = 0.f;
+#pragma unroll
+    for (int j = 0; j < JG; ++j) {
+      const float f = weight(sml[j][rr][0], M);
+      l += sml[j][rr][1] * f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] += so[j][rr][d0 + e] * f;
+    }
+  }
+  if (r >= t.rows) return;
+  const Pair pr(a, t, hk, t.m0 + r);
   const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) y[e] *= inv;
-  store_v<8>(a.o + (row * a.Hq + h) * D + d0, y);
+  for (int e = 0; e < 4; ++e) y[e] *= inv;
+  store_v<4>(a.o + (pr.row * a.Hq + pr.h) * D + d0, y);
   if (d0 == 0)
-    a.lse[int64_t(h) * a.N + row] =
+    a.lse[int64_t(pr.h) * a.N + pr.row] =
         l == 0.f ? -INFINITY : (M + __log2f(l)) * 0.69314718055994531f;
 }
 
@@ -522,35 +986,75 @@ __global__ __launch_bounds__(256) void tree_mask_kernel(int B, int N, const int3
 // --------------------------------------------------------------------------
 // launches
 // --------------------------------------------------------------------------
+constexpr int kFewWaves = 2;
+// Pairs per entry up to which the kernel for few pairs is used
+constexpr int kFewPairs = 32;
+
 struct TreePlan {
-  int tiles, target;
-  int64_t blocks;        // workgroups: runs there can be, over all KV heads
-  size_t o_bytes, bytes;
+  bool many;
+  int R, tiles, groups;
+  size_t o_bytes, ml_bytes, bytes;
 };
 
+// Two workgroups to a CU; no more than there are units, if the longest
+// sequence is known.
+static int tree_groups(const mv_cache_shape& c, const mv_tree_attn_shape& s, int64_t tiles) {
+  const int64_t groups = 2 * kNumCu;
+  if (s.max_len <= 0) return int(groups);
+  return int(std::min(groups, tiles * c.n_heads_kv * ((int64_t(s.max_len) + kUnit - 1) / kUnit)));
+}
+
 static TreePlan tree_plan(const mv_cache_shape& c, const mv_tree_attn_shape& s) {
-  constexpr int R = 32;
   TreePlan p;
   const int G = s.n_heads_q / c.n_heads_kv;
-  p.tiles = int(int64_t(s.n_rows) * G / R) + s.n_batch;
-  // Two workgroups to a CU, four of them in turn; not more than there are
-  // units if the longest sequence is known.
-  int64_t target = 4 * kNumCu;
-  if (s.max_len > 0)
-    target = std::min(target, int64_t(p.tiles) * c.n_heads_kv * ((s.max_len + kUnit - 1) / kUnit));
-  p.target = int(std::max<int64_t>(1, target));
-  p.blocks = int64_t(p.target) + int64_t(p.tiles) * c.n_heads_kv;
-  p.o_bytes = size_t(p.blocks) * R * c.head_dim * 4;
-  p.bytes = p.o_bytes + size_t(p.blocks) * R * 2 * 4;
+  const int64_t pairs = int64_t(s.n_rows) * G;
+  p.many = pairs > int64_t(kFewPairs) * s.n_batch;
+  p.R = p.many ? 128 : 32;
+  p.tiles = int(pairs / p.R) + s.n_batch;
+  p.groups = tree_groups(c, s, p.tiles);
+  p.o_bytes = size_t(2 * p.groups) * p.R * c.head_dim * 4;
+  p.ml_bytes = size_t(2 * p.groups) * p.R * 2 * 4;
+  p.bytes = p.o_bytes + p.ml_bytes + size_t(1 + p.tiles) * 8;
   return p;
 }
 
+// What any call of at most this many rows and entries needs: which kernel it
+// takes depends on both.
 size_t tree_attn_ws_bytes(const mv_cache_shape& c, const mv_tree_attn_shape& s) {
-  return tree_plan(c, s).bytes;
+  const int G = s.n_heads_q / c.n_heads_kv;
+  const size_t tiles = size_t(int64_t(s.n_rows) * G / 32) + s.n_batch;
+  const int64_t groups = tree_groups(c, s, int64_t(tiles));
+  return size_t(2 * groups) * 128 * (c.head_dim + 2) * 4 + (1 + tiles) * 8;
 }
 
-int64_t tree_attn_blocks(const mv_cache_shape& c, const mv_tree_attn_shape& s) {
-  return tree_plan(c, s).blocks;
+// Tile places past which the deal does not fit its LDS
+bool tree_attn_fits(const mv_cache_shape& c, const mv_tree_attn_shape& s) {
+  const TreePlan p = tree_plan(c, s);
+  return p.tiles <= kChunks * (p.many ? 256 : 64 * kFewWaves);
+}
+
+template <int D>
+static hipError_t launch_tree(const TreePlan& p, TreeArgs a, hipStream_t stream) {
+  {
+    ProfScope prof("tree_attn", stream);
+    if (p.many)
+      hipLaunchKernelGGL((tree_many_kernel<D>), dim3(p.groups), dim3(256), 0, stream, a);
+    else
+      hipLaunchKernelGGL((tree_few_kernel<D, kFewWaves>), dim3(p.groups), dim3(64 * kFewWaves), 0,
+                         stream, a);
+  }
+  if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  // one workgroup's run is every tile
+  if (p.groups == 1) return hipSuccess;
+  ProfScope prof("tree_combine", stream);
+  const int tiles = p.tiles * a.Hkv;
+  if (p.many)
+    hipLaunchKernelGGL((tree_combine_kernel<D, 128, 1>), dim3(unsigned(tiles * (D / 8))), dim3(256),
+                       0, stream, a);
+  else
+    hipLaunchKernelGGL((tree_combine_kernel<D, 32, 4>), dim3(unsigned(tiles * (D / 8))), dim3(256),
+                       0, stream, a);
+  return hipGetLastError();
 }
 
 hipError_t launch_tree_attn(const mv_cache_shape& cs, const CacheDev& cd, int layer,
@@ -565,8 +1069,10 @@ hipError_t launch_tree_attn(const mv_cache_shape& cs, const CacheDev& cd, int la
   a.v = cd.v + plane;
   a.o = static_cast<u16*>(o);
   a.lse = lse;
-  a.part_o = static_cast<float*>(ws);
-  a.part_ml = reinterpret_cast<float*>(static_cast<char*>(ws) + p.o_bytes);
+  char* w = static_cast<char*>(ws);
+  a.part_o = reinterpret_cast<float*>(w);
+  a.part_ml = reinterpret_cast<float*>(w + p.o_bytes);
+  a.plan = reinterpret_cast<int64_t*>(w + p.o_bytes + p.ml_bytes);
   a.table = cd.table;
   a.len = cd.len;
   a.ids = ids;
@@ -583,31 +1089,9 @@ hipError_t launch_tree_attn(const mv_cache_shape& cs, const CacheDev& cd, int la
   a.max_pages = cs.max_pages;
   a.psl = cd.psl;
   a.tiles = p.tiles;
-  a.target = p.target;
+  a.groups = p.groups;
   a.scale_log2 = scale * 1.4426950408889634f;
-  const int combine = p.tiles * cs.n_heads_kv;
-  if (cs.head_dim == 128) {
-    {
-      ProfScope prof("tree_attn", stream);
-      hipLaunchKernelGGL((tree_attn_kernel<128, 2>), dim3(unsigned(p.blocks)), dim3(128), 0,
-                         stream, a);
-    }
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    ProfScope prof("tree_combine", stream);
-    hipLaunchKernelGGL((tree_combine_kernel<128, 32>), dim3(unsigned(combine * 2)), dim3(256), 0,
-                       stream, a);
-  } else {
-    {
-      ProfScope prof("tree_attn", stream);
-      hipLaunchKernelGGL((tree_attn_kernel<64, 2>), dim3(unsigned(p.blocks)), dim3(128), 0, stream,
-                         a);
-    }
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    ProfScope prof("tree_combine", stream);
-    hipLaunchKernelGGL((tree_combine_kernel<64, 32>), dim3(unsigned(combine)), dim3(256), 0,
-                       stream, a);
-  }
-  return hipGetLastError();
+  return cs.head_dim == 128 ? launch_tree<128>(p, a, stream) : launch_tree<64>(p, a, stream);
 }
 
 hipError_t launch_tree_mask(int B, int N, const int32_t* ptr, const int32_t* parent, int words,
