@@ -33,7 +33,7 @@ struct TreeArgs {
   float* lse;
   float* part_o;       // [2 * groups][R][D] unnormalised
   float* part_ml;      // [2 * groups][R][2] maximum (base 2, scaled), sum
-  int64_t* plan;       // [1 + tiles]: units of a KV head, then each place's first unit
+  struct TreeJoin* join;   // [groups]
   const int32_t* table;
   const int32_t* len;
   const int32_t* ids;
@@ -46,13 +46,22 @@ struct TreeArgs {
   float scale_log2;
 };
 
+// What is to be joined of the tile that begins in workgroup g's run and goes on
+// in the next ones': its first segment is at `slot`, run g + j's at 2 (g + j).
+struct TreeJoin {
+  int rows;            // pairs of the tile; 0: nothing begins in g and goes on
+  int m0, r0, hk;      // first pair, the entry's first row of q, KV head
+  int runs, slot;
+  int pad[2];
+};
+
 constexpr int kUnit = 64;       // keys of a unit of work
 constexpr int kPlanB = 512;     // entries whose sizes are held in LDS
 constexpr int kChunks = 256;    // blocks of tile places whose first unit is held in LDS
 
 struct TreeShared {
   int ptr[kPlanB + 1];
-  int len[kPlanB];
+  int id[kPlanB], len[kPlanB];
   int tmp[17];
   int64_t first[kChunks + 1];   // first unit of each BLOCK of places
   int pre[257];                 // of one of them: each place's first unit, from there
@@ -82,8 +91,7 @@ __device__ __forceinline__ int first_place(int64_t r, int b, int G) {
   return int(r * G / R) + b;
 }
 
-__device__ __forceinline__ int entry_len(const TreeArgs& a, int b) {
-  const int id = a.ids[b];
+__device__ __forceinline__ int entry_len(const TreeArgs& a, int id) {
   return unsigned(id) < unsigned(a.n_seqs)
              ? int(min(int64_t(max(a.len[id], 0)), int64_t(a.max_pages) << a.psl)) : 0;
 }
@@ -108,7 +116,7 @@ __device__ __forceinline__ Tile tile_of(const TreeArgs& a, const TreeShared& s, 
     t.rows = 0;
     return t;
   }
-  const int L = lds ? s.len[lo] : entry_len(a, lo);
+  const int L = lds ? s.len[lo] : entry_len(a, a.ids[lo]);
   t.c = L - t.n;
   const int last = (t.m0 + t.rows - 1) / a.G;
   t.kmax = a.tree ? L : max(0, t.c + last + 1);
@@ -121,16 +129,25 @@ __device__ __forceinline__ Tile uniform(const Tile& t) {
           uniform(t.kmax)};
 }
 
+// The kernel's arguments read again from where they were passed: outside the
+// loops over keys, so that they do not take scalar registers inside them.
+__device__ __forceinline__ const TreeArgs& again() {
+  typedef __attribute__((address_space(4))) const TreeArgs args;
+  uint64_t p = reinterpret_cast<uint64_t>((const args*)__builtin_amdgcn_kernarg_segment_ptr());
+  asm volatile("" : "+s"(p));
+  return *(const TreeArgs*)(const args*)p;
+}
+
 // The deal: every workgroup works out the same one from the lengths.
 template <int R, int BLOCK>
 struct Deal {
-  const TreeArgs& a;
   TreeShared& s;
   int chunk;           // the BLOCK of places that s.pre is of
   int64_t units;       // of one KV head
   int64_t per;         // of a workgroup
 
   __device__ __forceinline__ int64_t scan(int j, int64_t first) {
+    const TreeArgs& a = again();
     const int u = j * BLOCK + threadIdx.x;
     const int mine = u < a.tiles ? tile_of<R>(a, s, u).units() : 0;
     int total;
@@ -139,16 +156,19 @@ struct Deal {
     const int before = block_scan<BLOCK>(mine, s.tmp, total);
     s.pre[threadIdx.x] = before;
     if (threadIdx.x == 0) s.pre[BLOCK] = total;
-    if (blockIdx.x == 0 && u < a.tiles) a.plan[1 + u] = first + before;
     chunk = j;
     return first + total;
   }
 
-  __device__ __forceinline__ Deal(const TreeArgs& args, TreeShared& sh) : a(args), s(sh) {
+  __device__ __forceinline__ explicit Deal(TreeShared& sh) : s(sh) {
+    const TreeArgs& a = again();
     if (a.B <= kPlanB) {
       for (int b = threadIdx.x; b <= a.B; b += BLOCK) {
         s.ptr[b] = min(max(a.ptr[b], 0), a.N);
-        if (b < a.B) s.len[b] = entry_len(a, b);
+        if (b < a.B) {
+          s.id[b] = a.ids[b];
+          s.len[b] = entry_len(a, s.id[b]);
+        }
       }
     }
     __syncthreads();
@@ -159,15 +179,35 @@ struct Deal {
       sum = scan(j, sum);
     }
     if (threadIdx.x == 0) s.first[chunks] = sum;
-    if (blockIdx.x == 0 && threadIdx.x == 0) a.plan[0] = sum;
     units = uniform(sum);
     per = max(int64_t(1), (units * a.Hkv + a.groups - 1) / a.groups);
     __syncthreads();
   }
 
+  __device__ __forceinline__ int id_of(int b) const {
+    const TreeArgs& a = again();
+    return uniform(a.B <= kPlanB ? s.id[b] : a.ids[b]);
+  }
+
+  // For the join: the segment of this run that a tile's other segments follow
+  // (p: its first unit, of run `run` from `begin` on)
+  __device__ __forceinline__ void note(const Tile& t, int hk, int run, int64_t begin, int64_t p,
+                                       int unit, bool whole) const {
+    if (unit != 0 || whole || threadIdx.x != 0) return;
+    const TreeArgs& a = again();
+    TreeJoin j{};
+    j.rows = t.rows;
+    j.m0 = t.m0;
+    j.r0 = t.r0;
+    j.hk = hk;
+    j.runs = int((p + t.units() - 1) / per) - run + 1;
+    j.slot = 2 * run + (p != begin);
+    a.join[run] = j;
+  }
+
   // The place that holds unit p of a KV head, and which of its units that is.
   __device__ __forceinline__ void find(int64_t p, int& place, int& unit) {
-    int lo = 0, hi = (a.tiles + BLOCK - 1) / BLOCK;
+    int lo = 0, hi = (again().tiles + BLOCK - 1) / BLOCK;
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (s.first[mid] <= p) lo = mid; else hi = mid;
@@ -343,19 +383,29 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
   __shared__ float sm[NW][R], sl[NW][R];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int c = lane & 31, g = lane >> 5;
-  Deal<R, BLOCK> deal(a, sh);
+  Deal<R, BLOCK> deal(sh);
   const int run = run_of_block(a.groups);
   const int64_t begin = run * deal.per;
   const int64_t end = min(begin + deal.per, deal.units * a.Hkv);
+  if (tid == 0) again().join[run].rows = 0;
   const int ps = 1 << a.psl;
-  const int lrow = lane / (D / 8), lpos = lane % (D / 8);
-  const uint32_t lds0 = lds_addr(&buf[wave][0]);
+  // A load's LR rows lie in one page; its address is scalar but for one of
+  // 16 / LR offsets per lane (the chunks' permutation has a period of 16 rows).
+  constexpr int NO = 16 / LR;
+  uint32_t voff[NO];
+#pragma unroll
+  for (int j = 0; j < NO; ++j) {
+    const int r = lane / (D / 8);
+    voff[j] = uint32_t(r * D * 2 + ((lane % (D / 8) ^ kv_swz<D>(j * LR + r)) << 4));
+  }
+  const int wv = uniform(wave);
+  const uint32_t lds0 = lds_addr(&buf[0][0]) + wv * 4 * TB;
 
   for (int64_t p = begin; p < end;) {
     const int hk = uniform(int(p / deal.units));
     int place, unit;
     deal.find(p - hk * deal.units, place, unit);
-    const Tile t = uniform(tile_of<R>(a, sh, place));
+    const Tile t = uniform(tile_of<R>(again(), sh, place));
     const int units = t.units();
     const int n_units = int(min(int64_t(units - unit), end - p));
 
@@ -378,32 +428,31 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
     const int k_begin = unit * kUnit;
     const int k_end = int(min(int64_t(t.kmax), int64_t(unit + n_units) * kUnit));
     const int nt = k_end > k_begin ? (k_end - k_begin + 31) / 32 : 0;
-    const int todo = nt > wave ? (nt - wave + NW - 1) / NW : 0;
-    auto key_of = [&](int x) { return k_begin + (wave + x * NW) * 32; };
+    const int todo = nt > wv ? (nt - wv + NW - 1) / NW : 0;
+    auto key_of = [&](int x) { return k_begin + (wv + x * NW) * 32; };
     const int last = t.kmax - 1;
     const int64_t page_bytes = int64_t(a.Hkv) * ps * D * 2;
     const char* kb = reinterpret_cast<const char*>(a.k) + int64_t(hk) * ps * D * 2;
     const char* vb = reinterpret_cast<const char*>(a.v) + int64_t(hk) * ps * D * 2;
     PageRing pages{nullptr, lds_addr(&pg[wave][0]), &pg[wave][0], 0, a.n_pages, a.psl};
     if (todo > 0) {
-      pages.row = a.table + int64_t(a.ids[t.b]) * a.max_pages;
+      pages.row = again().table + int64_t(deal.id_of(t.b)) * again().max_pages;
       pages.start(key_of(0), last);
       wait_loads<0>();
     }
-    // Tile x of this wave into buffer x & 1.  Keys past the last read the last
-    // (a load's rows lie in one page; what is past it is masked).
+    // Tile x of this wave into buffer x & 1.  Rows past the last key are read
+    // from the last key's page (what they hold is masked).
     auto issue = [&](int x) {
       const int key0 = key_of(x);
       pages.ahead(key0 >> a.psl, last);
       const uint32_t kl = lds0 + uint32_t(x & 1) * TB;
 #pragma unroll
       for (int j = 0; j < NI; ++j) {
-        const int64_t page = pages.get(min(key0 + j * LR, last) >> a.psl);
-        const int r = j * LR + lrow;
-        const uint32_t off = uint32_t(min(key0 + r, last) & (ps - 1)) * (D * 2) +
-                             uint32_t((lpos ^ kv_swz<D>(r)) << 4);
-        lds_load16s(uniform_ptr(kb + page * page_bytes), off, kl + j * 1024);
-        lds_load16s(uniform_ptr(vb + page * page_bytes), off, kl + 2 * TB + j * 1024);
+        const int key = key0 + j * LR;
+        const int64_t at = pages.get(min(key, last) >> a.psl) * page_bytes +
+                           (key & (ps - 1)) * (D * 2);
+        lds_load16s(kb + at, voff[j % NO], kl + j * 1024);
+        lds_load16s(vb + at, voff[j % NO], kl + 2 * TB + j * 1024);
       }
     };
     if (todo > 0) issue(0);
@@ -541,6 +590,7 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
         }
       }
     }
+    deal.note(t, hk, run, begin, p, unit, whole);
     __syncthreads();
     p += n_units;
   }
@@ -562,33 +612,40 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
   __shared__ TreeShared sh;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int c = lane & 31, g = lane >> 5;
-  Deal<R, BLOCK> deal(a, sh);
+  Deal<R, BLOCK> deal(sh);
   const int run = run_of_block(a.groups);
   const int64_t begin = run * deal.per;
   const int64_t end = min(begin + deal.per, deal.units * a.Hkv);
+  if (tid == 0) again().join[run].rows = 0;
   const int ps = 1 << a.psl;
-  const int lrow = lane / (D / 8), lpos = lane % (D / 8);
+  // A load's LR rows lie in one page (pages hold multiples of 16 rows), and
+  // their chunks' permutation does not depend on which load of the tile it is:
+  // one offset per lane serves all, the rest of the address is scalar.
+  const int wv = uniform(wave), lrow = lane / (D / 8);
+  const uint32_t voff = uint32_t(lrow * D * 2 + ((lane % (D / 8) ^ kv_swz<D>(wv * LR + lrow)) << 4));
+  const uint32_t ldsK = lds_addr(&sKb[0][0]) + wv * 1024, ldsV = lds_addr(&sVb[0][0]) + wv * 1024;
 
   for (int64_t p = begin; p < end;) {
     const int hk = uniform(int(p / deal.units));
     int place, unit;
     deal.find(p - hk * deal.units, place, unit);
-    const Tile t = uniform(tile_of<R>(a, sh, place));
+    const Tile t = uniform(tile_of<R>(again(), sh, place));
     const int units = t.units();
     const int n = int(min(int64_t(units - unit), end - p));   // 64-key tiles of the segment
 
     const int my = wave * 32 + c;
     const bool qok = my < t.rows;
     // this lane's pair, worked out again where it is needed rather than held
-    auto pair = [&]() {
+    auto pair = [&](const TreeArgs& b) {
       int m = t.m0 + (my < t.rows ? my : 0);
       asm volatile("" : "+v"(m));
-      return Pair(a, t, hk, m);
+      return Pair(b, t, hk, m);
     };
     bf16x8 qf[KS];
     {
-      const Pair mine = pair();
-      const u16* qp = a.q + (mine.row * a.Hq + mine.h) * D + g * 8;
+      const TreeArgs& b = again();
+      const Pair mine = pair(b);
+      const u16* qp = b.q + (mine.row * b.Hq + mine.h) * D + g * 8;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
         qf[ks] = as_bf16x8(qok ? ld16(qp + ks * 16) : make_uint4(0, 0, 0, 0));
@@ -602,46 +659,43 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
 
     const int key_base = unit * BK;
     const int last = t.kmax - 1;
-    const int64_t page_bytes = int64_t(a.Hkv) * ps * D * 2;
+    const uint32_t page_rows = uint32_t(a.Hkv) * ps;   // (a pool of 2^32 rows is past any memory)
     const char* kb = reinterpret_cast<const char*>(a.k) + int64_t(hk) * ps * D * 2;
     const char* vb = reinterpret_cast<const char*>(a.v) + int64_t(hk) * ps * D * 2;
     PageRing pages{nullptr, lds_addr(&pg[wave][0]), &pg[wave][0], 0, a.n_pages, a.psl};
     const bool keys = t.kmax > 0;   // block-uniform
     if (keys) {
-      pages.row = a.table + int64_t(a.ids[t.b]) * a.max_pages;
+      pages.row = again().table + int64_t(deal.id_of(t.b)) * again().max_pages;
       pages.start(key_base, last);
       wait_loads<0>();
     }
-    // 64-key tile x of one tensor into the LDS tile at `lds`
-    auto issue = [&](const char* base, int x, uint32_t lds) {
-      const int key0 = key_base + x * BK;
+    // The rows (of the layer's pool, from the KV head's first) that this wave
+    // loads of tile x.  Rows past the last key are read from the last key's page
+    // (what they hold is masked).
+    auto locate = [&](int x, uint32_t (&at)[NL]) {
 #pragma unroll
       for (int j = 0; j < NL; ++j) {
-        const int r0 = (j * 4 + wave) * LR, r = r0 + lrow;
-        const int64_t page = pages.get(min(key0 + r0, last) >> a.psl);
-        const uint32_t off = uint32_t(min(key0 + r, last) & (ps - 1)) * (D * 2) +
-                             uint32_t((lpos ^ kv_swz<D>(r)) << 4);
-        lds_load16s(uniform_ptr(base + page * page_bytes), off,
-                    lds + uint32_t(j * 4 + wave) * 1024);
+        const int key = key_base + x * BK + (j * 4 + wv) * LR;
+        at[j] = uint32_t(pages.get(min(key, last) >> a.psl)) * page_rows + (key & (ps - 1));
       }
     };
-    auto issue_k = [&](int x) { issue(kb, x, lds_addr(&sKb[x & 1][0])); };
-    // V runs a tile behind K, so it is V's tile that leaves a window for good
-    // (K needs the next one 15 tiles later at the earliest)
-    auto issue_v = [&](int x) {
-      pages.ahead((key_base + x * BK) >> a.psl, last);
-      issue(vb, x, lds_addr(&sVb[x & 1][0]));
+    auto issue = [&](const char* base, const uint32_t (&at)[NL], uint32_t lds) {
+#pragma unroll
+      for (int j = 0; j < NL; ++j)
+        lds_load16s(base + uint64_t(at[j]) * (D * 2), voff, lds + j * 4096);
     };
-    auto kfrag = [&](int x, int j) {
-      return ld_row_swz<D>(&sKb[x & 1][0], (j & 1) * 32 + c, (j >> 1) * 2 + g);
+    uint32_t at_v[NL], at_k[NL];   // of the V tile and of the K tile to be asked for next
+    auto kfrag = [&](int buf, int j) {
+      return ld_row_swz<D>(&sKb[buf][0], (j & 1) * 32 + c, (j >> 1) * 2 + g);
     };
     const int clear = a.tree ? t.c : t.c + t.m0 / a.G + 1;   // keys every row of the tile sees
     auto masked = [&](int x) { return key_base + x * BK + BK > min(clear, t.kmax); };
     auto seen = [&](int x, int kb2) {   // of keys 32 kb2 .. + 32 of tile x
       const int key0 = key_base + x * BK + kb2 * 32, m = t.kmax - key0;
       const uint32_t in = m >= 32 ? ~0u : m <= 0 ? 0u : (1u << m) - 1u;
-      const Pair mine = pair();
-      return seen32(a, t, mine.row, mine.i, key0) & in;
+      const TreeArgs& b = again();
+      const Pair mine = pair(b);
+      return seen32(b, t, mine.row, mine.i, key0) & in;
     };
     f32x16 sc[2][2];   // scores of tile x in sc[x & 1]
     auto mask_tile = [&](f32x16 (&s)[2], int x) {
@@ -700,8 +754,7 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
     };
     // Values that are not finite in a masked tile (see the kernel for few
     // pairs): added where they are seen, then made 0.
-    auto odd_values = [&](const f32x16 (&s)[2], int x) __attribute__((always_inline)) {
-      char* sV = &sVb[x & 1][0];
+    auto odd_values = [&](const f32x16 (&s)[2], int x, char* sV) __attribute__((always_inline)) {
       bool odd = false;
 #pragma unroll
       for (int j = 0; j < NL; ++j) odd |= odd16(sV + (j * 4 + wave) * 1024 + lane * 16);
@@ -729,9 +782,12 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
     bf16x8 pf[4];
     float psum_a = 0.f;
     if (keys) {
-      issue_k(0);
-      if (n > 1) issue_k(1);
-      issue_v(0);
+      locate(0, at_v);
+      issue(kb, at_v, ldsK);
+      issue(vb, at_v, ldsV);
+      locate(min(1, n - 1), at_v);
+      if (n > 1) issue(kb, at_v, ldsK + TB);
+      locate(min(2, n - 1), at_k);
       wait_loads<0>();
       __syncthreads();
 #pragma unroll
@@ -763,20 +819,20 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
       // K of tile x and V of tile x - 1
       wait_loads<0>();
       __syncthreads();
-      if (x + 2 < n) issue_k(x + 2);
-      if (next) issue_v(x + 1);
+      if (x + 2 < n) issue(kb, at_k, ldsK + P * TB);
+      if (next) issue(vb, at_v, ldsV + (P ^ 1) * TB);
       const float mu = m_off();
       float psum = psum_a;
       {
         bf16x8 kr[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) kr[j] = kfrag(x + 1, j);
+        for (int j = 0; j < 4; ++j) kr[j] = kfrag(P ^ 1, j);
         float q[16];
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int j = 0; j < 2 * KS; ++j) {
           nxt[j & 1] = mfma32(kr[j & 3], qf[j >> 1], j < 2 ? f32x16{} : nxt[j & 1]);
-          if (j + 4 < 2 * KS) kr[j & 3] = kfrag(x + 1, j + 4);
+          if (j + 4 < 2 * KS) kr[j & 3] = kfrag(P ^ 1, j + 4);
           constexpr int NS = 2 * KS;
           const int i0 = 16 * j / NS, i1 = 16 * (j + 1) / NS;
 #pragma unroll
@@ -794,11 +850,18 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
       }
       if (__any(!(psum <= 65536.f) || (qok && m_run == -INFINITY))) slow_tile(cur, pf, psum);
       l_run += psum;
-      if (masked(x)) odd_values(cur, x);
+      if (masked(x)) odd_values(cur, x, &sVb[P][0]);
       if (next) mask_tile(nxt, x + 1);
+      // the tiles asked for after the next barrier: V follows K
+#pragma unroll
+      for (int j = 0; j < NL; ++j) at_v[j] = at_k[j];
+      if (x + 3 < n) {
+        pages.ahead((key_base + (x + 3) * BK) >> a.psl, last);
+        locate(x + 3, at_k);
+      }
       {
         const float mu1 = m_off();
-        const char* sV = &sVb[x & 1][0];
+        const char* sV = &sVb[P][0];
         auto vfrag = [&](int st) { return ld_tr_swz<D>(sV, (st / DB) * 16, (st % DB) * 32); };
         bf16x8 vr[4];
 #pragma unroll
@@ -837,10 +900,11 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
     }
     const float l = l_run + __shfl_xor(l_run, 32);
     if (qok) {
-      const Pair mine = pair();
+      const TreeArgs& b = again();
+      const Pair mine = pair(b);
       if (n == units) {
         const float inv = l == 0.f ? 0.f : 1.f / l;   // l is 0 where no key was seen
-        u16* op = a.o + (mine.row * a.Hq + mine.h) * D;
+        u16* op = b.o + (mine.row * b.Hq + mine.h) * D;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -849,11 +913,11 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
                 make_uint2(pack2(oacc[db][q4 * 4 + 0] * inv, oacc[db][q4 * 4 + 1] * inv),
                            pack2(oacc[db][q4 * 4 + 2] * inv, oacc[db][q4 * 4 + 3] * inv));
         if (g == 0)
-          a.lse[int64_t(mine.h) * a.N + mine.row] =
+          b.lse[int64_t(mine.h) * b.N + mine.row] =
               l == 0.f ? -INFINITY : (m_run + __log2f(l)) * 0.69314718055994531f;
       } else {
         const int64_t s = (2 * int64_t(run) + (p != begin)) * R + my;
-        float* op = a.part_o + s * D;
+        float* op = b.part_o + s * D;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -862,60 +926,59 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
                 make_float4(oacc[db][q4 * 4 + 0], oacc[db][q4 * 4 + 1], oacc[db][q4 * 4 + 2],
                             oacc[db][q4 * 4 + 3]);
         if (g == 0) {
-          a.part_ml[s * 2] = m_run;
-          a.part_ml[s * 2 + 1] = l;
+          b.part_ml[s * 2] = m_run;
+          b.part_ml[s * 2 + 1] = l;
         }
       }
     }
+    deal.note(t, hk, run, begin, p, unit, n == units);
     __syncthreads();   // the tiles are read before the next segment's loads
     p += n;
   }
 }
 
 // --------------------------------------------------------------------------
-// Joins the segments of a tile, in their order: block (tile place, KV head,
-// RG pairs), JG groups of D / 4 threads to a pair, each for every JG-th segment.
+// Joins the segments of a tile, in their order: block (run, RG pairs), JG
+// groups of D / 4 threads to a pair, each for every JG-th segment.
 // --------------------------------------------------------------------------
 template <int D, int R, int JG>
-__global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a) {
-  constexpr int TD = D / 4, RG = 256 / (TD * JG), NG = R / RG;
+__global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
+  constexpr int TD = D / 4, RG = 256 / (TD * JG), NG = R / RG, U = 4;
   __shared__ float so[JG][RG][D], sml[JG][RG][2];
-  int x = blockIdx.x;
-  const int rg = x % NG;
-  x /= NG;
-  const int hk = x % a.Hkv, place = x / a.Hkv;
-  const int64_t units = a.plan[0], first = a.plan[1 + place];
-  const int64_t next = place + 1 < a.tiles ? a.plan[2 + place] : units;
-  const int64_t per = max(int64_t(1), (units * a.Hkv + a.groups - 1) / a.groups);
-  const int64_t p0 = hk * units + first, p1 = hk * units + next;
-  // the runs that hold units [p0, p1)
-  const int64_t g0 = p0 / per, g1 = p1 > p0 ? (p1 - 1) / per : g0;
-  if (g0 == g1) return;   // written whole (or no tile)
+  const int run = blockIdx.x / NG, rg = blockIdx.x % NG;
+  const TreeJoin jn = a.join[run];
+  if (rg * RG >= jn.rows) return;   // block-uniform
   const int d0 = (threadIdx.x % TD) * 4, rr = threadIdx.x / TD % RG, jg = threadIdx.x / (TD * RG);
   const int r = rg * RG + rr;
-  // the entry, from its place
-  int lo = 0, hi = a.B;
-  auto at = [&](int b) { return min(max(a.ptr[b], 0), a.N); };
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (first_place<R>(at(mid), mid, a.G) <= place) lo = mid; else hi = mid;
-  }
-  Tile t;
-  t.r0 = at(lo);
-  t.m0 = (place - first_place<R>(t.r0, lo, a.G)) * R;
-  t.rows = min(R, (at(lo + 1) - t.r0) * a.G - t.m0);
-  if (rg * RG >= t.rows) return;   // block-uniform
-  auto slot = [&](int64_t run) { return (2 * run + (run * per < p0)) * R + r; };
   float M = -INFINITY, l = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
-  if (r < t.rows) {
-    for (int64_t j = g0 + jg; j <= g1; j += JG) M = fmaxf(M, a.part_ml[2 * slot(j)]);
-#pragma unroll 4
-    for (int64_t j = g0 + jg; j <= g1; j += JG) {
-      const int64_t s = slot(j);
-      const float f = weight(a.part_ml[2 * s], M);
-      l += a.part_ml[2 * s + 1] * f;
-      const float4 u = *reinterpret_cast<const float4*>(a.part_o + s * D + d0);
-      y[0] += u.x * f, y[1] += u.y * f, y[2] += u.z * f, y[3] += u.w * f;
+  if (r < jn.rows) {
+    for (int j0 = jg; j0 < jn.runs; j0 += JG * U) {
+      float mj[U], lj[U];
+      float4 oj[U];
+#pragma unroll
+      for (int x = 0; x < U; ++x) {
+        const int j = min(j0 + x * JG, jn.runs - 1);
+        const int64_t s = int64_t(j == 0 ? jn.slot : 2 * (run + j)) * R + r;
+        const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * s);
+        mj[x] = ml.x;
+        lj[x] = ml.y;
+        oj[x] = *reinterpret_cast<const float4*>(a.part_o + s * D + d0);
+      }
+      float Mn = M;
+#pragma unroll
+      for (int x = 0; x < U; ++x) Mn = fmaxf(Mn, mj[x]);   // (a repeated last one does not matter)
+      float f = weight(M, Mn);
+      l *= f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] *= f;
+#pragma unroll
+      for (int x = 0; x < U; ++x) {
+        if (j0 + x * JG >= jn.runs) break;
+        f = weight(mj[x], Mn);
+        l += lj[x] * f;
+        y[0] += oj[x].x * f, y[1] += oj[x].y * f, y[2] += oj[x].z * f, y[3] += oj[x].w * f;
+      }
+      M = Mn;
     }
   }
   if (JG > 1) {
@@ -938,8 +1001,10 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeArgs a) {
       for (int e = 0; e < 4; ++e) y[e] += so[j][rr][d0 + e] * f;
     }
   }
-  if (r >= t.rows) return;
-  const Pair pr(a, t, hk, t.m0 + r);
+  if (r >= jn.rows) return;
+  Tile t{};
+  t.r0 = jn.r0;
+  const Pair pr(a, t, jn.hk, jn.m0 + r);
   const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
   for (int e = 0; e < 4; ++e) y[e] *= inv;
@@ -1014,7 +1079,7 @@ static TreePlan tree_plan(const mv_cache_shape& c, const mv_tree_attn_shape& s) 
   p.groups = tree_groups(c, s, p.tiles);
   p.o_bytes = size_t(2 * p.groups) * p.R * c.head_dim * 4;
   p.ml_bytes = size_t(2 * p.groups) * p.R * 2 * 4;
-  p.bytes = p.o_bytes + p.ml_bytes + size_t(1 + p.tiles) * 8;
+  p.bytes = p.o_bytes + p.ml_bytes + sizeof(TreeJoin) * p.groups;
   return p;
 }
 
@@ -1022,9 +1087,8 @@ static TreePlan tree_plan(const mv_cache_shape& c, const mv_tree_attn_shape& s) 
 // takes depends on both.
 size_t tree_attn_ws_bytes(const mv_cache_shape& c, const mv_tree_attn_shape& s) {
   const int G = s.n_heads_q / c.n_heads_kv;
-  const size_t tiles = size_t(int64_t(s.n_rows) * G / 32) + s.n_batch;
-  const int64_t groups = tree_groups(c, s, int64_t(tiles));
-  return size_t(2 * groups) * 128 * (c.head_dim + 2) * 4 + (1 + tiles) * 8;
+  const int64_t groups = tree_groups(c, s, int64_t(s.n_rows) * G / 32 + s.n_batch);
+  return size_t(2 * groups) * 128 * (c.head_dim + 2) * 4 + sizeof(TreeJoin) * groups;
 }
 
 // Tile places past which the deal does not fit its LDS
@@ -1047,13 +1111,16 @@ static hipError_t launch_tree(const TreePlan& p, TreeArgs a, hipStream_t stream)
   // one workgroup's run is every tile
   if (p.groups == 1) return hipSuccess;
   ProfScope prof("tree_combine", stream);
-  const int tiles = p.tiles * a.Hkv;
-  if (p.many)
-    hipLaunchKernelGGL((tree_combine_kernel<D, 128, 1>), dim3(unsigned(tiles * (D / 8))), dim3(256),
-                       0, stream, a);
-  else
-    hipLaunchKernelGGL((tree_combine_kernel<D, 32, 4>), dim3(unsigned(tiles * (D / 8))), dim3(256),
-                       0, stream, a);
+  // Tiles in many segments (fewer tiles than runs) are joined by four groups of
+  // threads a pair, each with every fourth segment.
+  const bool wide = int64_t(p.tiles) * a.Hkv * 2 < p.groups;
+#define MV_JOIN(R, JG)                                                                        \
+  hipLaunchKernelGGL((tree_join_kernel<D, R, JG>), dim3(unsigned(p.groups * (R * JG * D / 1024))), \
+                     dim3(256), 0, stream, a)
+  if (p.many && wide) MV_JOIN(128, 4);
+  else if (p.many) MV_JOIN(128, 1);
+  else MV_JOIN(32, 4);
+#undef MV_JOIN
   return hipGetLastError();
 }
 
@@ -1072,7 +1139,7 @@ hipError_t launch_tree_attn(const mv_cache_shape& cs, const CacheDev& cd, int la
   char* w = static_cast<char*>(ws);
   a.part_o = reinterpret_cast<float*>(w);
   a.part_ml = reinterpret_cast<float*>(w + p.o_bytes);
-  a.plan = reinterpret_cast<int64_t*>(w + p.o_bytes + p.ml_bytes);
+  a.join = reinterpret_cast<TreeJoin*>(w + p.o_bytes + p.ml_bytes);
   a.table = cd.table;
   a.len = cd.len;
   a.ids = ids;
