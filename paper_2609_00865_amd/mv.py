@@ -279,8 +279,16 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
+# torch.cuda.current_stream() builds a Stream object by way of several device
+# look-ups (4 us of the host's time); the handle alone is one call.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _stream(stream=None):
     if stream is None:
+        if _raw_stream is not None and torch.cuda.is_initialized():
+            return _raw_stream(_device())
         stream = torch.cuda.current_stream()
     return stream.cuda_stream
 
@@ -771,12 +779,11 @@ def sdcc_lambda(step: int, total_steps: int, lambda_max: float = 0.1,
 # ---------------------------------------------------------------------------
 def _need(t, dtype, what, shape=None, contiguous=True):
     """A CUDA tensor of the current device with the given type (and shape)."""
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or not t.is_cuda:
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or not t.is_cuda:
         raise ValueError(f"{what}: expected a {dtype} CUDA tensor")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{what} is on {t.device}, the current device is "
-                         f"cuda:{torch.cuda.current_device()}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if t.get_device() != _device():
+        raise ValueError(f"{what} is on {t.device}, the current device is cuda:{_device()}")
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{what}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
     if contiguous and not t.is_contiguous():
         raise ValueError(f"{what}: expected a contiguous tensor")
@@ -786,22 +793,25 @@ def _token_stride(t, what):
     """Elements from one token of t [n, heads, d] to the next; a token's own
     elements lie together."""
     n, h, d = t.shape
-    if (d > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != d):
+    token, head, one = t.stride()
+    if (d > 1 and one != 1) or (h > 1 and head != d):
         raise ValueError(f"{what}: the heads of a token must lie together")
-    return t.stride(0) if n > 1 else h * d
+    return token if n > 1 else h * d
 
 
 def _use(stream, *ts):
     """The stream's handle; tensors made here on the current stream are kept
     from reuse until `stream` is done with them."""
+    if stream is None:
+        return _stream()
     cur = torch.cuda.current_stream()
-    if stream is not None and stream != cur:
+    if stream != cur:
         # what this call allocated may be a block whose last use is queued there
         stream.wait_stream(cur)
         for t in ts:
             if t is not None:
                 t.record_stream(stream)
-    return _stream(stream)
+    return stream.cuda_stream
 
 
 class RopeAxes:
@@ -819,12 +829,14 @@ class RopeAxes:
         if self.n_axes > 8:
             raise ValueError("axis_map: at most 8 axes")
         self.c = RopeAxesC(self.rotary_dim, self.n_axes, self.theta, (ctypes.c_uint8 * 128)(*axis))
+        self._ref = ctypes.byref(self.c)
 
 
 def _rope_pos(rope, pos, n):
-    if pos is None or pos.dim() != 2 or pos.shape[0] < rope.n_axes:
+    _need(pos, torch.int32, "pos")
+    shape = pos.shape
+    if len(shape) != 2 or shape[0] < rope.n_axes or shape[1] != n:
         raise ValueError(f"pos: expected [{rope.n_axes}, {n}] position ids")
-    _need(pos, torch.int32, "pos", (pos.shape[0], n))
 
 
 def rope_axes(x, pos, rope: RopeAxes, inverse: bool = False, out=None, stream=None):
@@ -832,18 +844,19 @@ def rope_axes(x, pos, rope: RopeAxes, inverse: bool = False, out=None, stream=No
     elements apart) rotated by pos int32 [n_axes, n]; ``inverse``: by the
     negative angles, which is the backward.  ``out`` may be x."""
     _need(x, torch.bfloat16, "x", contiguous=False)
-    if x.dim() != 3 or x.shape[2] != rope.head_dim:
+    shape = x.shape
+    if len(shape) != 3 or shape[2] != rope.head_dim:
         raise ValueError(f"x: expected [n, heads, {rope.head_dim}]")
-    _rope_pos(rope, pos, x.shape[0])
+    n, heads, d = shape
+    _rope_pos(rope, pos, n)
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        handle = _use(stream, out)
+        out = torch.empty(shape, dtype=torch.bfloat16, device=x.device)
+        handle, out_stride = _use(stream, out), heads * d
     else:
-        _need(out, torch.bfloat16, "out", x.shape, contiguous=False)
-        handle = _stream(stream)
-    check(mv_rope_axes(ctypes.byref(rope.c), x.shape[0], x.shape[1], x.shape[2], _ptr(x),
-                       _token_stride(x, "x"), _ptr(pos), -1 if inverse else 1, _ptr(out),
-                       _token_stride(out, "out"), handle))
+        _need(out, torch.bfloat16, "out", shape, contiguous=False)
+        handle, out_stride = _stream(stream), _token_stride(out, "out")
+    check(mv_rope_axes(rope._ref, n, heads, d, x.data_ptr(), _token_stride(x, "x"),
+                       pos.data_ptr(), -1 if inverse else 1, out.data_ptr(), out_stride, handle))
     return out
 
 
@@ -862,8 +875,8 @@ class PagedCache:
         self.shape = CacheShape(n_layers, n_pages, page_size, n_heads_kv, head_dim, n_seqs,
                                 max_pages)
         dev = torch.device(device)
-        if dev.type == "cuda" and dev.index not in (None, torch.cuda.current_device()):
-            raise ValueError(f"device {dev} is not the current one")
+        if dev.type != "cuda" or dev.index not in (None, torch.cuda.current_device()):
+            raise ValueError(f"device {dev} is not the current CUDA device")
         # a shape that the library refuses is refused before anything is allocated
         if not mv_cache_compact_workspace_bytes(ctypes.byref(self.shape), 0):
             check(mv_cache_reset(ctypes.byref(self.shape), None, None))
@@ -875,13 +888,15 @@ class PagedCache:
         self.page_refs, self._ctl = i32(n_pages), i32(4)
         self.c = CacheC(_ptr(self.k), _ptr(self.v), _ptr(self.page_table), _ptr(self.seq_len),
                         _ptr(self.page_refs), _ptr(self._ctl))
+        self._dev, self.head_dim = self.k.get_device(), int(head_dim)
+        self._refs = (ctypes.byref(self.shape), ctypes.byref(self.c))
         self.reset(stream)
 
     def _args(self):
-        if self.k.device.index != torch.cuda.current_device():
-            raise ValueError(f"the cache is on {self.k.device}, the current device is "
-                             f"cuda:{torch.cuda.current_device()}")
-        return ctypes.byref(self.shape), ctypes.byref(self.c)
+        if self._dev != _device():
+            raise ValueError(f"the cache is on cuda:{self._dev}, the current device is "
+                             f"cuda:{_device()}")
+        return self._refs
 
     def reset(self, stream=None) -> None:
         """Every sequence empty, every page free."""
@@ -911,6 +926,7 @@ def _need_ids(t, what, n=None):
     _need(t, torch.int32, what)
     if t.dim() != 1 or (n is not None and t.numel() != n):
         raise ValueError(f"{what}: expected a vector" + (f" of {n}" if n is not None else ""))
+    return t.numel()
 
 
 def cache_reserve(cache: PagedCache, seq_ids, new_ptr, n_new: int, stream=None):
@@ -941,13 +957,13 @@ def cache_write(cache: PagedCache, layer: int, slot, k, v, rope: Optional[RopeAx
         _rope_pos(rope, pos, n)
     check(mv_cache_write(*cache._args(), int(layer), n, _ptr(slot), _ptr(k),
                          _token_stride(k, "k"), _ptr(v), _token_stride(v, "v"),
-                         ctypes.byref(rope.c) if rope is not None else None,
+                         rope._ref if rope is not None else None,
                          _ptr(pos) if rope is not None else None, _stream(stream)))
 
 
 def cache_workspace(cache: PagedCache, n: int) -> torch.Tensor:
     """Workspace of cache_fork and cache_compact calls of up to n entries."""
-    nbytes = int(mv_cache_compact_workspace_bytes(ctypes.byref(cache.shape), int(n)))
+    nbytes = int(mv_cache_compact_workspace_bytes(cache._refs[0], int(n)))
     return torch.empty(nbytes, dtype=torch.uint8, device=cache.k.device)
 
 
@@ -955,19 +971,19 @@ def cache_fork(cache: PagedCache, src, dst, share: bool = True, workspace=None,
                stream=None) -> None:
     """Sequence dst[e] (empty) becomes a copy of src[e], its full pages shared
     (or copied too)."""
-    _need_ids(src, "src")
-    _need_ids(dst, "dst", src.numel())
-    ws = workspace if workspace is not None else cache_workspace(cache, src.numel())
-    check(mv_cache_fork(*cache._args(), src.numel(), _ptr(src), _ptr(dst), 1 if share else 0,
-                        _ptr(ws), ws.numel(), _use(stream, ws if workspace is None else None)))
+    n = _need_ids(src, "src")
+    _need_ids(dst, "dst", n)
+    ws = workspace if workspace is not None else cache_workspace(cache, n)
+    check(mv_cache_fork(*cache._args(), n, src.data_ptr(), dst.data_ptr(), 1 if share else 0,
+                        ws.data_ptr(), ws.numel(),
+                        _use(stream, ws if workspace is None else None)))
 
 
 def cache_compact(cache: PagedCache, src, dst, span_ptr, spans, workspace=None,
                   stream=None) -> None:
     """Evict rows spans[span_ptr[e] : span_ptr[e+1]] (int32 [n, 2], half-open)
     of src[e]; dst[e] (src[e] itself, or empty) holds the others in order."""
-    _need_ids(src, "src")
-    n = src.numel()
+    n = _need_ids(src, "src")
     _need_ids(dst, "dst", n)
     _need_ids(span_ptr, "span_ptr", n + 1)
     _need(spans, torch.int32, "spans")
@@ -1022,34 +1038,38 @@ def tree_attn(cache: PagedCache, layer: int, q, seq_ids, row_ptr, tree=None,
     (o [n, Hq, d] bf16, lse fp32 [Hq, n]).  ``tree`` (from tree_mask): which
     new rows a row sees; otherwise itself and those before it.  ``max_len``:
     the longest sequence expected, if known.  ``out``: (o, lse) to write."""
-    s = cache.shape
     _need(q, torch.bfloat16, "q")
-    if q.dim() != 3 or q.shape[2] != s.head_dim:
-        raise ValueError(f"q: expected [n, heads, {s.head_dim}]")
-    _need_ids(seq_ids, "seq_ids")
-    B = seq_ids.numel()
+    dims = q.shape
+    if len(dims) != 3 or dims[2] != cache.head_dim:
+        raise ValueError(f"q: expected [n, heads, {cache.head_dim}]")
+    n, heads, _ = dims
+    B = _need_ids(seq_ids, "seq_ids")
     _need_ids(row_ptr, "row_ptr", B + 1)
+    words = 0
     if tree is not None:
         _need(tree, torch.int32, "tree")
-        if tree.dim() != 2 or tree.shape[0] != q.shape[0] or tree.shape[1] < 1:
+        if tree.dim() != 2 or tree.shape[0] != n or tree.shape[1] < 1:
             raise ValueError("tree: expected [n, words], at least one word")
-    shape = _tree_attn_shape(q, B, tree, scale, max_len)
-    made = []
+        words = tree.shape[1]
+    shape = ctypes.byref(TreeAttnShape(B, n, heads, words, int(max_len),
+                                       float(scale) if scale else 0.0))
+    refs, dev = cache._args(), q.device
     if out is None:
-        o = torch.empty_like(q)
-        lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
-        made += [o, lse]
+        o = torch.empty(dims, dtype=torch.bfloat16, device=dev)
+        lse = torch.empty((heads, n), dtype=torch.float32, device=dev)
     else:
         o, lse = out
-        _need(o, torch.bfloat16, "o", q.shape)
-        _need(lse, torch.float32, "lse", (q.shape[1], q.shape[0]))
-    if workspace is None:
-        n = int(mv_tree_attn_workspace_bytes(ctypes.byref(s), ctypes.byref(shape)))
-        workspace = torch.empty(n, dtype=torch.uint8, device=q.device)
-        made.append(workspace)
-    check(mv_tree_attn(*cache._args(), int(layer), ctypes.byref(shape), _ptr(seq_ids),
-                       _ptr(row_ptr), _ptr(tree), _ptr(q), _ptr(o), _ptr(lse), _ptr(workspace),
-                       workspace.numel(), _use(stream, *made)))
+        _need(o, torch.bfloat16, "o", dims)
+        _need(lse, torch.float32, "lse", (heads, n))
+    ws = workspace
+    if ws is None:
+        ws = torch.empty(int(mv_tree_attn_workspace_bytes(refs[0], shape)), dtype=torch.uint8,
+                         device=dev)
+    handle = _stream(stream) if stream is None else _use(
+        stream, *((o, lse) if out is None else ()), *((ws,) if workspace is None else ()))
+    check(mv_tree_attn(*refs, int(layer), shape, seq_ids.data_ptr(), row_ptr.data_ptr(),
+                       _ptr(tree), q.data_ptr(), o.data_ptr(), lse.data_ptr(), ws.data_ptr(),
+                       ws.numel(), handle))
     return o, lse
 
 
