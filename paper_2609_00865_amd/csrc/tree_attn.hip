@@ -59,19 +59,6 @@ constexpr int kUnit = 64;       // keys of a unit of work
 constexpr int kPlanB = 512;     // entries whose sizes are held in LDS
 constexpr int kChunks = 256;    // blocks of tile places whose first unit is held in LDS
 
-struct TreeShared {
-  int ptr[kPlanB + 1];
-  int id[kPlanB], len[kPlanB];
-  int tmp[17];
-  int64_t first[kChunks + 1];   // first unit of each BLOCK of places
-  int pre[257];                 // of one of them: each place's first unit, from there
-};
-
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ int64_t uniform(int64_t x) {
-  return int64_t(uint64_t(uint32_t(uniform(int(x >> 32)))) << 32 | uint32_t(uniform(int(x))));
-}
-
 // One tile: the entry, its first pair, and the keys any of its rows may see.
 struct Tile {
   int b, n, c;      // entry, its rows, its context rows (negative: absent rows)
@@ -83,6 +70,20 @@ struct Tile {
     return rows ? max(1, (kmax + kUnit - 1) / kUnit) : 0;
   }
 };
+
+struct TreeShared {
+  int ptr[kPlanB + 1];
+  int id[kPlanB], len[kPlanB];
+  int tmp[17];
+  int64_t first[kChunks + 1];   // first unit of each BLOCK of places
+  Tile tile;                    // where a run begins
+  int unit;
+};
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  return int64_t(uint64_t(uint32_t(uniform(int(x >> 32)))) << 32 | uint32_t(uniform(int(x))));
+}
 
 // Entry b's first tile place: places of entries never overlap, because
 // ceil(n G / R) <= floor((r + n) G / R) - floor(r G / R) + 1.
@@ -96,31 +97,37 @@ __device__ __forceinline__ int entry_len(const TreeArgs& a, int id) {
              ? int(min(int64_t(max(a.len[id], 0)), int64_t(a.max_pages) << a.psl)) : 0;
 }
 
+__device__ __forceinline__ int first_row(const TreeArgs& a, const TreeShared& s, int b) {
+  return a.B <= kPlanB ? s.ptr[b] : min(max(a.ptr[b], 0), a.N);
+}
+
+// The tile of entry b whose first pair is m0.
+template <int R>
+__device__ __forceinline__ Tile tile_at(const TreeArgs& a, const TreeShared& s, int b, int m0) {
+  Tile t;
+  t.b = b;
+  t.r0 = first_row(a, s, b);
+  t.n = max(0, first_row(a, s, b + 1) - t.r0);
+  t.m0 = m0;
+  t.rows = m0 >= 0 ? max(0, min(R, t.n * a.G - m0)) : 0;
+  t.kmax = t.c = 0;
+  if (t.rows == 0) return t;
+  const int L = a.B <= kPlanB ? s.len[b] : entry_len(a, a.ids[b]);
+  t.c = L - t.n;
+  const int last = (m0 + t.rows - 1) / a.G;
+  t.kmax = a.tree ? L : max(0, t.c + last + 1);
+  return t;
+}
+
+// The tile of place u (no rows: there is none).
 template <int R>
 __device__ __forceinline__ Tile tile_of(const TreeArgs& a, const TreeShared& s, int u) {
-  const bool lds = a.B <= kPlanB;
-  auto at = [&](int b) { return lds ? s.ptr[b] : min(max(a.ptr[b], 0), a.N); };
   int lo = 0, hi = a.B;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
-    if (first_place<R>(at(mid), mid, a.G) <= u) lo = mid; else hi = mid;
+    if (first_place<R>(first_row(a, s, mid), mid, a.G) <= u) lo = mid; else hi = mid;
   }
-  Tile t;
-  t.b = lo;
-  t.r0 = at(lo);
-  t.n = max(0, at(lo + 1) - t.r0);
-  t.m0 = (u - first_place<R>(t.r0, lo, a.G)) * R;
-  t.rows = t.m0 >= 0 ? min(R, t.n * a.G - t.m0) : 0;
-  t.kmax = t.c = 0;
-  if (t.rows <= 0) {
-    t.rows = 0;
-    return t;
-  }
-  const int L = lds ? s.len[lo] : entry_len(a, a.ids[lo]);
-  t.c = L - t.n;
-  const int last = (t.m0 + t.rows - 1) / a.G;
-  t.kmax = a.tree ? L : max(0, t.c + last + 1);
-  return t;
+  return tile_at<R>(a, s, lo, (u - first_place<R>(first_row(a, s, lo), lo, a.G)) * R);
 }
 
 // A tile's fields are the same in every lane: held in scalar registers.
@@ -138,30 +145,40 @@ __device__ __forceinline__ const TreeArgs& again() {
   return *(const TreeArgs*)(const args*)p;
 }
 
-// The deal: every workgroup works out the same one from the lengths.
+__device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {   // of what mostly fits 32 bits
+  if (((x | y) >> 32) == 0) return uint32_t(x) / uint32_t(y);
+  return x / y;
+}
+
+// The deal: every workgroup works out the same one from the lengths, and
+// walks its own run of it, segment by segment.
 template <int R, int BLOCK>
 struct Deal {
   TreeShared& s;
-  int chunk;           // the BLOCK of places that s.pre is of
   int64_t units;       // of one KV head
-  int64_t per;         // of a workgroup
+  int64_t per;         // of a run
+  int64_t begin, end;  // this run, over all KV heads
+  // the segment: its first unit among all, tile, KV head, first unit of the
+  // tile, units of the segment and of the tile
+  int64_t p;
+  Tile t;
+  int hk, unit, n, of;
+  int run;
 
-  __device__ __forceinline__ int64_t scan(int j, int64_t first) {
+  // The units of places [j BLOCK, (j + 1) BLOCK) and before each of them.
+  __device__ __forceinline__ void scan(int j, Tile& mine, int& before, int& total) {
     const TreeArgs& a = again();
     const int u = j * BLOCK + threadIdx.x;
-    const int mine = u < a.tiles ? tile_of<R>(a, s, u).units() : 0;
-    int total;
+    mine = Tile{};
+    if (u < a.tiles) mine = tile_of<R>(a, s, u);
     // (a tile has fewer than 2^25 units: BLOCK of them do not pass 2^31 unless
     // the caches are past any memory, in which case the rows are unspecified)
-    const int before = block_scan<BLOCK>(mine, s.tmp, total);
-    s.pre[threadIdx.x] = before;
-    if (threadIdx.x == 0) s.pre[BLOCK] = total;
-    chunk = j;
-    return first + total;
+    before = block_scan<BLOCK>(mine.units(), s.tmp, total);
   }
 
-  __device__ __forceinline__ explicit Deal(TreeShared& sh) : s(sh) {
+  __device__ __forceinline__ Deal(TreeShared& sh, int r) : s(sh), run(r) {
     const TreeArgs& a = again();
+    if (threadIdx.x == 0) a.join[run].rows = 0;
     if (a.B <= kPlanB) {
       for (int b = threadIdx.x; b <= a.B; b += BLOCK) {
         s.ptr[b] = min(max(a.ptr[b], 0), a.N);
@@ -173,60 +190,92 @@ struct Deal {
     }
     __syncthreads();
     const int chunks = (a.tiles + BLOCK - 1) / BLOCK;
+    Tile mine;
+    int before = 0, total;
     int64_t sum = 0;
     for (int j = 0; j < chunks; ++j) {
+      scan(j, mine, before, total);
       if (threadIdx.x == 0) s.first[j] = sum;
-      sum = scan(j, sum);
+      sum += total;
     }
-    if (threadIdx.x == 0) s.first[chunks] = sum;
     units = uniform(sum);
-    per = max(int64_t(1), (units * a.Hkv + a.groups - 1) / a.groups);
+    per = max(int64_t(1), quotient(units * a.Hkv + a.groups - 1, a.groups));
+    begin = run * per;
+    end = min(begin + per, units * a.Hkv);
+    p = begin;
+    if (p >= end) return;
+    hk = uniform(int(quotient(p, units)));
+    int64_t x = p - hk * units;
+    if (chunks > 1) {
+      __syncthreads();
+      int lo = 0, hi = chunks;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (s.first[mid] <= x) lo = mid; else hi = mid;
+      }
+      lo = uniform(lo);
+      x -= s.first[lo];
+      scan(lo, mine, before, total);
+    }
+    if (x >= before && x < before + mine.units()) {
+      s.tile = mine;
+      s.unit = int(x) - before;
+    }
     __syncthreads();
+    t = uniform(s.tile);
+    unit = uniform(s.unit);
+    of = t.units();
+    n = int(min(int64_t(of - unit), end - p));
   }
 
-  __device__ __forceinline__ int id_of(int b) const {
+  __device__ __forceinline__ bool done() const { return p >= end; }
+
+  // On to the next tile: of the entry, of the next entry that has rows, of the
+  // next KV head.
+  __device__ __forceinline__ void next() {
+    p += n;
+    if (p >= end) return;
     const TreeArgs& a = again();
-    return uniform(a.B <= kPlanB ? s.id[b] : a.ids[b]);
+    int b = t.b, m0 = t.m0 + R;
+    if (m0 >= t.n * a.G) {
+      m0 = 0;
+      do {
+        if (++b == a.B) {
+          b = 0;
+          if (++hk == a.Hkv) {   // (row_ptr not as it should be)
+            p = end;
+            return;
+          }
+        }
+      } while (uniform(first_row(a, s, b + 1)) <= uniform(first_row(a, s, b)));
+    }
+    t = uniform(tile_at<R>(a, s, b, m0));
+    unit = 0;
+    of = t.units();
+    n = int(min(int64_t(of), end - p));
   }
 
-  // For the join: the segment of this run that a tile's other segments follow
-  // (p: its first unit, of run `run` from `begin` on)
-  __device__ __forceinline__ void note(const Tile& t, int hk, int run, int64_t begin, int64_t p,
-                                       int unit, bool whole) const {
-    if (unit != 0 || whole || threadIdx.x != 0) return;
+  __device__ __forceinline__ bool whole() const { return n == of; }
+  // where the segment's partial result goes
+  __device__ __forceinline__ int64_t slot() const { return 2 * int64_t(run) + (p != begin); }
+
+  __device__ __forceinline__ const int32_t* pages() const {   // the sequence's row of the table
     const TreeArgs& a = again();
+    const int id = uniform(a.B <= kPlanB ? s.id[t.b] : a.ids[t.b]);
+    return a.table + int64_t(id) * a.max_pages;
+  }
+
+  // For the join: the segment that a tile's other segments follow
+  __device__ __forceinline__ void note() const {
+    if (unit != 0 || whole() || threadIdx.x != 0) return;
     TreeJoin j{};
     j.rows = t.rows;
     j.m0 = t.m0;
     j.r0 = t.r0;
     j.hk = hk;
-    j.runs = int((p + t.units() - 1) / per) - run + 1;
-    j.slot = 2 * run + (p != begin);
-    a.join[run] = j;
-  }
-
-  // The place that holds unit p of a KV head, and which of its units that is.
-  __device__ __forceinline__ void find(int64_t p, int& place, int& unit) {
-    int lo = 0, hi = (again().tiles + BLOCK - 1) / BLOCK;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (s.first[mid] <= p) lo = mid; else hi = mid;
-    }
-    const int j = uniform(lo);
-    const int64_t first = s.first[j];
-    if (j != chunk) {
-      __syncthreads();
-      scan(j, first);
-      __syncthreads();
-    }
-    const int x = int(p - first);
-    lo = 0, hi = BLOCK;   // the last place whose first unit is not past x
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (s.pre[mid] <= x) lo = mid; else hi = mid;
-    }
-    place = uniform(j * BLOCK + lo);
-    unit = uniform(x - s.pre[lo]);
+    j.runs = int(quotient(p + of - 1, per)) - run + 1;
+    j.slot = int(slot());
+    again().join[run] = j;
   }
 };
 
@@ -383,11 +432,7 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
   __shared__ float sm[NW][R], sl[NW][R];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int c = lane & 31, g = lane >> 5;
-  Deal<R, BLOCK> deal(sh);
-  const int run = run_of_block(a.groups);
-  const int64_t begin = run * deal.per;
-  const int64_t end = min(begin + deal.per, deal.units * a.Hkv);
-  if (tid == 0) again().join[run].rows = 0;
+  Deal<R, BLOCK> deal(sh, run_of_block(a.groups));
   const int ps = 1 << a.psl;
   // A load's LR rows lie in one page; its address is scalar but for one of
   // 16 / LR offsets per lane (the chunks' permutation has a period of 16 rows).
@@ -401,13 +446,9 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
   const int wv = uniform(wave);
   const uint32_t lds0 = lds_addr(&buf[0][0]) + wv * 4 * TB;
 
-  for (int64_t p = begin; p < end;) {
-    const int hk = uniform(int(p / deal.units));
-    int place, unit;
-    deal.find(p - hk * deal.units, place, unit);
-    const Tile t = uniform(tile_of<R>(again(), sh, place));
-    const int units = t.units();
-    const int n_units = int(min(int64_t(units - unit), end - p));
+  for (; !deal.done(); deal.next()) {
+    const Tile& t = deal.t;
+    const int hk = deal.hk;
 
     // Q^T as the B operand: lane holds pair c, dims ks*16 + g*8 .. + 8
     const bool qok = c < t.rows;
@@ -425,8 +466,8 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
     float m_run = -INFINITY, l_run = 0.f;
 
     // this segment's keys; wave w takes 32-key tiles w, w + NW, ...
-    const int k_begin = unit * kUnit;
-    const int k_end = int(min(int64_t(t.kmax), int64_t(unit + n_units) * kUnit));
+    const int k_begin = deal.unit * kUnit;
+    const int k_end = int(min(int64_t(t.kmax), int64_t(deal.unit + deal.n) * kUnit));
     const int nt = k_end > k_begin ? (k_end - k_begin + 31) / 32 : 0;
     const int todo = nt > wv ? (nt - wv + NW - 1) / NW : 0;
     auto key_of = [&](int x) { return k_begin + (wv + x * NW) * 32; };
@@ -436,7 +477,7 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
     const char* vb = reinterpret_cast<const char*>(a.v) + int64_t(hk) * ps * D * 2;
     PageRing pages{nullptr, lds_addr(&pg[wave][0]), &pg[wave][0], 0, a.n_pages, a.psl};
     if (todo > 0) {
-      pages.row = again().table + int64_t(deal.id_of(t.b)) * again().max_pages;
+      pages.row = deal.pages();
       pages.start(key_of(0), last);
       wait_loads<0>();
     }
@@ -555,8 +596,7 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
             make_float4(oacc[db][q4 * 4 + 0] * f, oacc[db][q4 * 4 + 1] * f,
                         oacc[db][q4 * 4 + 2] * f, oacc[db][q4 * 4 + 3] * f);
     __syncthreads();
-    const bool whole = n_units == units;
-    const int64_t slot = 2 * int64_t(run) + (p != begin);
+    const int64_t slot = deal.slot();
     for (int x = tid; x < t.rows * (D / 8); x += BLOCK) {
       const int r = x / (D / 8), d0 = (x % (D / 8)) * 8;
       float Mr = sm[0][r], l = 0.f;
@@ -571,7 +611,7 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[e] += q[e];
       }
-      if (whole) {
+      if (deal.whole()) {
         const Pair pr(a, t, hk, t.m0 + r);
         const float inv = l == 0.f ? 0.f : 1.f / l;   // l is 0 where no key was seen
 #pragma unroll
@@ -590,9 +630,8 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
         }
       }
     }
-    deal.note(t, hk, run, begin, p, unit, whole);
+    deal.note();
     __syncthreads();
-    p += n_units;
   }
 }
 
@@ -612,11 +651,7 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
   __shared__ TreeShared sh;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int c = lane & 31, g = lane >> 5;
-  Deal<R, BLOCK> deal(sh);
-  const int run = run_of_block(a.groups);
-  const int64_t begin = run * deal.per;
-  const int64_t end = min(begin + deal.per, deal.units * a.Hkv);
-  if (tid == 0) again().join[run].rows = 0;
+  Deal<R, BLOCK> deal(sh, run_of_block(a.groups));
   const int ps = 1 << a.psl;
   // A load's LR rows lie in one page (pages hold multiples of 16 rows), and
   // their chunks' permutation does not depend on which load of the tile it is:
@@ -625,16 +660,14 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
   const uint32_t voff = uint32_t(lrow * D * 2 + ((lane % (D / 8) ^ kv_swz<D>(wv * LR + lrow)) << 4));
   const uint32_t ldsK = lds_addr(&sKb[0][0]) + wv * 1024, ldsV = lds_addr(&sVb[0][0]) + wv * 1024;
 
-  for (int64_t p = begin; p < end;) {
-    const int hk = uniform(int(p / deal.units));
-    int place, unit;
-    deal.find(p - hk * deal.units, place, unit);
-    const Tile t = uniform(tile_of<R>(again(), sh, place));
-    const int units = t.units();
-    const int n = int(min(int64_t(units - unit), end - p));   // 64-key tiles of the segment
+  for (; !deal.done(); deal.next()) {
+    const Tile& t = deal.t;
+    const int hk = deal.hk, n = deal.n;   // n: 64-key tiles of the segment
 
     const int my = wave * 32 + c;
     const bool qok = my < t.rows;
+    // a wave without pairs loads its share of the tiles and computes nothing
+    const bool active = wv * 32 < t.rows;
     // this lane's pair, worked out again where it is needed rather than held
     auto pair = [&](const TreeArgs& b) {
       int m = t.m0 + (my < t.rows ? my : 0);
@@ -657,7 +690,7 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
       for (int r = 0; r < 16; ++r) oacc[db][r] = 0.f;
     float m_run = -INFINITY, l_run = 0.f;
 
-    const int key_base = unit * BK;
+    const int key_base = deal.unit * BK;
     const int last = t.kmax - 1;
     const uint32_t page_rows = uint32_t(a.Hkv) * ps;   // (a pool of 2^32 rows is past any memory)
     const char* kb = reinterpret_cast<const char*>(a.k) + int64_t(hk) * ps * D * 2;
@@ -665,7 +698,7 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
     PageRing pages{nullptr, lds_addr(&pg[wave][0]), &pg[wave][0], 0, a.n_pages, a.psl};
     const bool keys = t.kmax > 0;   // block-uniform
     if (keys) {
-      pages.row = again().table + int64_t(deal.id_of(t.b)) * again().max_pages;
+      pages.row = deal.pages();
       pages.start(key_base, last);
       wait_loads<0>();
     }
@@ -790,6 +823,8 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
       locate(min(2, n - 1), at_k);
       wait_loads<0>();
       __syncthreads();
+    }
+    if (keys && active) {
 #pragma unroll
       for (int j = 0; j < 2 * KS; ++j)
         sc[0][j & 1] = mfma32(kfrag(0, j), qf[j >> 1], j < 2 ? f32x16{} : sc[0][j & 1]);
@@ -822,8 +857,8 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
       if (x + 2 < n) issue(kb, at_k, ldsK + P * TB);
       if (next) issue(vb, at_v, ldsV + (P ^ 1) * TB);
       const float mu = m_off();
-      float psum = psum_a;
-      {
+      if (active) {
+        float psum = psum_a;
         bf16x8 kr[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) kr[j] = kfrag(P ^ 1, j);
@@ -847,11 +882,11 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
           }
           __builtin_amdgcn_sched_barrier(0);
         }
+        if (__any(!(psum <= 65536.f) || (qok && m_run == -INFINITY))) slow_tile(cur, pf, psum);
+        l_run += psum;
       }
-      if (__any(!(psum <= 65536.f) || (qok && m_run == -INFINITY))) slow_tile(cur, pf, psum);
-      l_run += psum;
       if (masked(x)) odd_values(cur, x, &sVb[P][0]);
-      if (next) mask_tile(nxt, x + 1);
+      if (next && active) mask_tile(nxt, x + 1);
       // the tiles asked for after the next barrier: V follows K
 #pragma unroll
       for (int j = 0; j < NL; ++j) at_v[j] = at_k[j];
@@ -859,7 +894,7 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
         pages.ahead((key_base + (x + 3) * BK) >> a.psl, last);
         locate(x + 3, at_k);
       }
-      {
+      if (active) {
         const float mu1 = m_off();
         const char* sV = &sVb[P][0];
         auto vfrag = [&](int st) { return ld_tr_swz<D>(sV, (st / DB) * 16, (st % DB) * 32); };
@@ -902,7 +937,7 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
     if (qok) {
       const TreeArgs& b = again();
       const Pair mine = pair(b);
-      if (n == units) {
+      if (deal.whole()) {
         const float inv = l == 0.f ? 0.f : 1.f / l;   // l is 0 where no key was seen
         u16* op = b.o + (mine.row * b.Hq + mine.h) * D;
 #pragma unroll
@@ -916,7 +951,7 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
           b.lse[int64_t(mine.h) * b.N + mine.row] =
               l == 0.f ? -INFINITY : (m_run + __log2f(l)) * 0.69314718055994531f;
       } else {
-        const int64_t s = (2 * int64_t(run) + (p != begin)) * R + my;
+        const int64_t s = deal.slot() * R + my;
         float* op = b.part_o + s * D;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
@@ -931,9 +966,8 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
         }
       }
     }
-    deal.note(t, hk, run, begin, p, unit, n == units);
+    deal.note();
     __syncthreads();   // the tiles are read before the next segment's loads
-    p += n;
   }
 }
 
