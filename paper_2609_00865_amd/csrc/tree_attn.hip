@@ -973,50 +973,54 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
 
 // --------------------------------------------------------------------------
 // Joins the segments of a tile, in their order: block (run, RG pairs), JG
-// groups of D / 4 threads to a pair, each for every JG-th segment.
+// groups of D / 8 threads to a pair, each for every JG-th segment.
 // --------------------------------------------------------------------------
 template <int D, int R, int JG>
 __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
-  constexpr int TD = D / 4, RG = 256 / (TD * JG), NG = R / RG, U = 4;
+  constexpr int TD = D / 8, RG = 256 / (TD * JG), NG = R / RG, U = 4;
   __shared__ float so[JG][RG][D], sml[JG][RG][2];
   const int run = blockIdx.x / NG, rg = blockIdx.x % NG;
   const TreeJoin jn = a.join[run];
   if (rg * RG >= jn.rows) return;   // block-uniform
-  const int d0 = (threadIdx.x % TD) * 4, rr = threadIdx.x / TD % RG, jg = threadIdx.x / (TD * RG);
+  const int d0 = (threadIdx.x % TD) * 8, rr = threadIdx.x / TD % RG, jg = threadIdx.x / (TD * RG);
   const int r = rg * RG + rr;
-  float M = -INFINITY, l = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
+  float M = -INFINITY, l = 0.f, y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   if (r < jn.rows) {
     for (int j0 = jg; j0 < jn.runs; j0 += JG * U) {
-      float mj[U], lj[U];
-      float4 oj[U];
+      float2 ml[U];
+      float4 oj[U][2];
 #pragma unroll
       for (int x = 0; x < U; ++x) {
         const int j = min(j0 + x * JG, jn.runs - 1);
         const int64_t s = int64_t(j == 0 ? jn.slot : 2 * (run + j)) * R + r;
-        const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * s);
-        mj[x] = ml.x;
-        lj[x] = ml.y;
-        oj[x] = *reinterpret_cast<const float4*>(a.part_o + s * D + d0);
+        ml[x] = *reinterpret_cast<const float2*>(a.part_ml + 2 * s);
+        oj[x][0] = *reinterpret_cast<const float4*>(a.part_o + s * D + d0);
+        oj[x][1] = *reinterpret_cast<const float4*>(a.part_o + s * D + d0 + 4);
       }
       float Mn = M;
 #pragma unroll
-      for (int x = 0; x < U; ++x) Mn = fmaxf(Mn, mj[x]);   // (a repeated last one does not matter)
+      for (int x = 0; x < U; ++x) Mn = fmaxf(Mn, ml[x].x);   // (the last one again does not matter)
       float f = weight(M, Mn);
       l *= f;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] *= f;
+      for (int e = 0; e < 8; ++e) y[e] *= f;
 #pragma unroll
       for (int x = 0; x < U; ++x) {
         if (j0 + x * JG >= jn.runs) break;
-        f = weight(mj[x], Mn);
-        l += lj[x] * f;
-        y[0] += oj[x].x * f, y[1] += oj[x].y * f, y[2] += oj[x].z * f, y[3] += oj[x].w * f;
+        f = weight(ml[x].x, Mn);
+        l += ml[x].y * f;
+        y[0] += oj[x][0].x * f, y[1] += oj[x][0].y * f;
+        y[2] += oj[x][0].z * f, y[3] += oj[x][0].w * f;
+        y[4] += oj[x][1].x * f, y[5] += oj[x][1].y * f;
+        y[6] += oj[x][1].z * f, y[7] += oj[x][1].w * f;
       }
       M = Mn;
     }
   }
   if (JG > 1) {
-    *reinterpret_cast<float4*>(&so[jg][rr][d0]) = make_float4(y[0], y[1], y[2], y[3]);
+    float* o = &so[jg][rr][d0];
+    *reinterpret_cast<float4*>(o) = make_float4(y[0], y[1], y[2], y[3]);
+    *reinterpret_cast<float4*>(o + 4) = make_float4(y[4], y[5], y[6], y[7]);
     if (d0 == 0) {
       sml[jg][rr][0] = M;
       sml[jg][rr][1] = l;
@@ -1026,13 +1030,14 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
 #pragma unroll
     for (int j = 1; j < JG; ++j) M = fmaxf(M, sml[j][rr][0]);
     l = 0.f;
-    y[0] = y[1] = y[2] = y[3] = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = 0.f;
 #pragma unroll
     for (int j = 0; j < JG; ++j) {
       const float f = weight(sml[j][rr][0], M);
       l += sml[j][rr][1] * f;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] += so[j][rr][d0 + e] * f;
+      for (int e = 0; e < 8; ++e) y[e] += so[j][rr][d0 + e] * f;
     }
   }
   if (r >= jn.rows) return;
@@ -1041,8 +1046,8 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
   const Pair pr(a, t, jn.hk, jn.m0 + r);
   const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) y[e] *= inv;
-  store_v<4>(a.o + (pr.row * a.Hq + pr.h) * D + d0, y);
+  for (int e = 0; e < 8; ++e) y[e] *= inv;
+  store_v<8>(a.o + (pr.row * a.Hq + pr.h) * D + d0, y);
   if (d0 == 0)
     a.lse[int64_t(pr.h) * a.N + pr.row] =
         l == 0.f ? -INFINITY : (M + __log2f(l)) * 0.69314718055994531f;
@@ -1145,15 +1150,17 @@ static hipError_t launch_tree(const TreePlan& p, TreeArgs a, hipStream_t stream)
   // one workgroup's run is every tile
   if (p.groups == 1) return hipSuccess;
   ProfScope prof("tree_combine", stream);
-  // Tiles in many segments (fewer tiles than runs) are joined by four groups of
-  // threads a pair, each with every fourth segment.
-  const bool wide = int64_t(p.tiles) * a.Hkv * 2 < p.groups;
+  // Tiles of many segments are joined by four groups of threads a pair, each
+  // with every fourth one; where there are few to a tile, blocks of four times
+  // the pairs (a quarter of the blocks) do it sooner.
+  const bool wide = p.groups >= 8 * int64_t(p.tiles) * a.Hkv;
 #define MV_JOIN(R, JG)                                                                        \
-  hipLaunchKernelGGL((tree_join_kernel<D, R, JG>), dim3(unsigned(p.groups * (R * JG * D / 1024))), \
+  hipLaunchKernelGGL((tree_join_kernel<D, R, JG>), dim3(unsigned(p.groups * (R * JG * D / 2048))), \
                      dim3(256), 0, stream, a)
   if (p.many && wide) MV_JOIN(128, 4);
   else if (p.many) MV_JOIN(128, 1);
-  else MV_JOIN(32, 4);
+  else if (wide) MV_JOIN(32, 4);
+  else MV_JOIN(32, 1);
 #undef MV_JOIN
   return hipGetLastError();
 }
