@@ -40,50 +40,74 @@ __global__ void cache_clear_counts_kernel(CacheDev a) {
   a.ctl[kCtlBad] = 0;
 }
 
-// Deals the lowest `need` free pages: take(q, page) for q = 0, 1, ...;
-// returns how many there were (at most need).  Every thread of the block
-// calls it; the hint is moved past the last page dealt.
-template <typename F>
-__device__ __forceinline__ int deal_pages(const CacheDev& a, int need, int* tmp, F take) {
-  int found = 0;
-  int64_t base = max(0, a.ctl[kCtlHint]) & ~3;
-  __syncthreads();   // the hint is read before it is moved
-  for (; found < need && base < a.n_pages; base += 4 * kPlan) {
-    const int64_t p = base + 4 * threadIdx.x;
-    int4 r = make_int4(1, 1, 1, 1);
-    if (p + 3 < a.n_pages) {
-      r = *reinterpret_cast<const int4*>(a.refs + p);
-    } else {
-      if (p < a.n_pages) r.x = a.refs[p];
-      if (p + 1 < a.n_pages) r.y = a.refs[p + 1];
-      if (p + 2 < a.n_pages) r.z = a.refs[p + 2];
-    }
-    const int f[4] = {r.x == 0, r.y == 0, r.z == 0, r.w == 0};
-    int total;
-    int q = found + block_scan<kPlan>(f[0] + f[1] + f[2] + f[3], tmp, total);
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      if (f[u] && q < need) {
-        take(q, int(p) + u);
-        if (q == need - 1) a.ctl[kCtlHint] = int(p) + u + 1;
-      }
-      q += f[u];
-    }
-    found = min(need, found + total);
-  }
-  if (found < need && threadIdx.x == 0) a.ctl[kCtlHint] = a.n_pages;
-  __syncthreads();
-  return found;
+// The holder counts of 4 pages per thread from `base` on (1 past the pool).
+__device__ __forceinline__ int4 refs_at(const CacheDev& a, int64_t base) {
+  const int64_t p = base + 4 * threadIdx.x;
+  if (p + 3 < a.n_pages) return *reinterpret_cast<const int4*>(a.refs + p);
+  int4 r = make_int4(1, 1, 1, 1);
+  if (p < a.n_pages) r.x = a.refs[p];
+  if (p + 1 < a.n_pages) r.y = a.refs[p + 1];
+  if (p + 2 < a.n_pages) r.z = a.refs[p + 2];
+  return r;
 }
 
-// The last e with pre[e] <= q, of n >= 1 ascending prefix sums (pre[0] = 0).
-__device__ __forceinline__ int entry_of(const int* pre, int n, int q) {
-  int lo = 0, hi = n;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (pre[mid] <= q) lo = mid; else hi = mid;
+// Where the search for free pages begins, and what it sees first: read when a
+// block starts, so that these loads wait beside those of the entries.
+struct Search {
+  int64_t base;
+  int4 refs;
+  __device__ __forceinline__ explicit Search(const CacheDev& a)
+      : base(max(0, a.ctl[kCtlHint]) & ~3), refs(refs_at(a, base)) {}
+};
+
+// The last e with pre[e] <= q, of n >= 1 ascending prefix sums (pre[0] = 0),
+// for four q at a time: their look-ups in LDS wait together.
+__device__ __forceinline__ void entries_of(const int* pre, int n, const int (&q)[4],
+                                           int (&e)[4]) {
+#pragma unroll
+  for (int u = 0; u < 4; ++u) e[u] = 0;
+  for (int step = 1 << (31 - __clz(n)); step; step >>= 1) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int x = e[u] + step;
+      if (x < n && pre[x] <= q[u]) e[u] = x;
+    }
   }
-  return lo;
+}
+
+// Deals the lowest `need` free pages to the n entries that pre divides:
+// take(q, entry, page) for q = 0, 1, ...; returns how many there were (at most need).  Every thread of the block
+// calls it; the hint is moved past the last page dealt.  (What take() stores
+// is not waited for.)
+template <typename F>
+__device__ __forceinline__ int deal_pages(const CacheDev& a, const int* pre, int n, int need,
+                                          const Search& from, int* tmp, F take) {
+  int found = 0;
+  int64_t base = from.base;
+  int4 r = from.refs;
+  while (found < need && base < a.n_pages) {
+    const int f[4] = {r.x == 0, r.y == 0, r.z == 0, r.w == 0};
+    int total;
+    int q[4], e[4];
+    q[0] = found + block_scan<kPlan>(f[0] + f[1] + f[2] + f[3], tmp, total);
+#pragma unroll
+    for (int u = 1; u < 4; ++u) q[u] = q[u - 1] + f[u - 1];
+    if (q[0] < need && (f[0] | f[1] | f[2] | f[3])) {
+      entries_of(pre, n, q, e);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (!f[u] || q[u] >= need) continue;
+        const int page = int(base) + 4 * threadIdx.x + u;
+        take(q[u], e[u], page);
+        if (q[u] == need - 1) a.ctl[kCtlHint] = page + 1;
+      }
+    }
+    found = min(need, found + total);
+    base += 4 * kPlan;
+    if (found < need && base < a.n_pages) r = refs_at(a, base);
+  }
+  if (found < need && threadIdx.x == 0) a.ctl[kCtlHint] = a.n_pages;
+  return found;
 }
 
 // --------------------------------------------------------------------------
@@ -94,17 +118,27 @@ struct Grow {   // what entry e asks for
   bool bad, over;   // malformed; more rows than the table can hold
 };
 
-__device__ __forceinline__ Grow grow_of(const CacheDev& a, const int32_t* ids, const int32_t* ptr,
-                                        int n_new, const int* claim, int e) {
+// Entry e's words and its sequence's length, as read
+struct GrowIn {
+  int s, r0, r1, len;
+  GrowIn() = default;
+  __device__ __forceinline__ GrowIn(const CacheDev& a, const int32_t* ids, const int32_t* ptr,
+                                    int e)
+      : s(ids[e]), r0(ptr[e]), r1(ptr[e + 1]),
+        len(unsigned(s) < unsigned(a.n_seqs) ? a.length(s) : 0) {}
+};
+
+__device__ __forceinline__ Grow grow_of(const CacheDev& a, const GrowIn& in, int n_new,
+                                        const int* claim, int e) {
   Grow g{};
-  g.s = ids[e];
-  g.r0 = ptr[e];
-  const int r1 = ptr[e + 1];
-  const bool in = unsigned(g.s) < unsigned(a.n_seqs);
-  g.bad = g.r0 < 0 || r1 < g.r0 || r1 > n_new || (!in && g.s != -1) || (in && claim[g.s] != e);
-  if (g.bad || !in) return g;
-  g.rows = r1 - g.r0;
-  g.len = a.length(g.s);
+  g.s = in.s;
+  g.r0 = in.r0;
+  const bool inside = unsigned(g.s) < unsigned(a.n_seqs);
+  g.bad = in.r0 < 0 || in.r1 < in.r0 || in.r1 > n_new || (!inside && g.s != -1) ||
+          (inside && claim[g.s] != e);
+  if (g.bad || !inside) return g;
+  g.rows = in.r1 - in.r0;
+  g.len = in.len;
   g.have = a.pages_of(g.len);
   const int64_t want = (int64_t(g.len) + g.rows + (1 << a.psl) - 1) >> a.psl;
   g.over = want > a.max_pages;
@@ -120,40 +154,48 @@ __global__ __launch_bounds__(kPlan) void cache_reserve_kernel(CacheDev a, int n,
                                                               int32_t* __restrict__ pos) {
   __shared__ int claim[kMaxSeqs];
   __shared__ int pre[kMaxSeqs + 1];
+  __shared__ Grow grow[kPlan];          // of the kPlan entries at hand
   __shared__ int tmp[kPlan / 64 + 1];
   __shared__ int cnt[2], cut_e;
   const int tid = threadIdx.x;
+  const GrowIn in = n > 0 ? GrowIn(a, ids, ptr, min(tid, n - 1)) : GrowIn{};
+  const Search from(a);
   for (int t = tid; t < n_new; t += kPlan) {
     slot[t] = -1;
     if (pos) pos[t] = -1;
   }
   for (int s = tid; s < a.n_seqs; s += kPlan) claim[s] = n;
   if (tid == 0) cnt[0] = cnt[1] = 0, cut_e = -1;
-  __syncthreads();
-  for (int e = tid; e < n; e += kPlan)
-    if (unsigned(ids[e]) < unsigned(a.n_seqs)) atomicMin(&claim[ids[e]], e);
-  __syncthreads();
+  lds_barrier();
+  for (int e = tid; e < n; e += kPlan) {
+    const int x = e == tid ? in.s : ids[e];
+    if (unsigned(x) < unsigned(a.n_seqs)) atomicMin(&claim[x], e);
+  }
+  lds_barrier();
   int need = 0;
   for (int e0 = 0; e0 < n; e0 += kPlan) {
     const int e = e0 + tid;
-    int want = 0, total;
+    Grow g{};
+    int total;
     if (e < n) {
-      const Grow g = grow_of(a, ids, ptr, n_new, claim, e);
-      want = g.need;
+      g = grow_of(a, e0 == 0 ? in : GrowIn(a, ids, ptr, e), n_new, claim, e);
       if (g.bad) atomicAdd(&cnt[1], 1);
       if (g.over) atomicAdd(&cnt[0], 1);
     }
-    const int before = need + block_scan<kPlan>(want, tmp, total);
+    if (e0 == 0) grow[tid] = g;
+    const int before = need + block_scan<kPlan>(g.need, tmp, total);
     if (e < n) pre[e] = before;
     need += total;   // at most the table's entries: sequences are named once
   }
   if (tid == 0) pre[n] = need;
-  __syncthreads();
-  const int found = deal_pages(a, need, tmp, [&](int q, int page) {
-    const int e = entry_of(pre, n, q), s = ids[e];
-    a.table[int64_t(s) * a.max_pages + a.pages_of(a.length(s)) + q - pre[e]] = page;
+  lds_barrier();
+  const int found = deal_pages(a, pre, n, need, from, tmp, [&](int q, int e, int page) {
+    const int s = e < kPlan ? grow[e].s : ids[e];
+    const int have = e < kPlan ? grow[e].have : a.pages_of(a.length(s));
+    a.table[int64_t(s) * a.max_pages + have + q - pre[e]] = page;
     a.refs[page] = 1;
   });
+  __syncthreads();   // table entries dealt, slots cleared
   if (found < need) {
     // the one entry that some but not all of its pages were dealt to
     for (int e = tid; e < n; e += kPlan) {
@@ -174,21 +216,25 @@ __global__ __launch_bounds__(kPlan) void cache_reserve_kernel(CacheDev a, int n,
     }
     __syncthreads();
   }
-  // rows of an accepted entry, a wave to an entry
+  // the rows and new lengths of accepted entries, a wave to an entry
   const int lane = tid & 63, mask = (1 << a.psl) - 1;
-  for (int e = tid >> 6; e < n; e += kPlan / 64) {
-    const Grow g = grow_of(a, ids, ptr, n_new, claim, e);
-    if (g.need > 0 && pre[e + 1] > found) continue;
-    for (int i = lane; i < g.rows; i += 64) {
-      const int r = g.len + i;
-      slot[g.r0 + i] = (a.page(g.s, r >> a.psl) << a.psl) + (r & mask);
-      if (pos) pos[g.r0 + i] = r;
+  for (int e0 = 0; e0 < n; e0 += kPlan) {
+    if (e0 > 0) {
+      __syncthreads();
+      if (e0 + tid < n)
+        grow[tid] = grow_of(a, GrowIn(a, ids, ptr, e0 + tid), n_new, claim, e0 + tid);
+      __syncthreads();
     }
-  }
-  __syncthreads();
-  for (int e = tid; e < n; e += kPlan) {
-    const Grow g = grow_of(a, ids, ptr, n_new, claim, e);
-    if (g.rows > 0 && (g.need == 0 || pre[e + 1] <= found)) a.len[g.s] = g.len + g.rows;
+    for (int e = e0 + (tid >> 6); e < min(n, e0 + kPlan); e += kPlan / 64) {
+      const Grow g = grow[e - e0];
+      if (g.rows == 0 || (g.need > 0 && pre[e + 1] > found)) continue;
+      for (int i = lane; i < g.rows; i += 64) {
+        const int r = g.len + i;
+        slot[g.r0 + i] = (a.page(g.s, r >> a.psl) << a.psl) + (r & mask);
+        if (pos) pos[g.r0 + i] = r;
+      }
+      if (lane == 0) a.len[g.s] = g.len + g.rows;
+    }
   }
   if (tid == 0) {
     a.ctl[kCtlNoPages] += cnt[0];
@@ -205,15 +251,14 @@ struct MoveRec {   // entry e, as planned
   int len, new_len;
   int keep;        // pages that stay (dst == src) or are shared
   int n_new;       // new pages behind them
-  int off;         // their first place in the list of new pages
   int span0, n_spans;
   int old_pages;   // pages of src
-  int pad;
 };
 
 struct MoveWs {
   int* head;       // [4]: new pages dealt
   MoveRec* rec;    // [n]
+  int* off;        // [n]: its new pages' first place in the list of them
   int2* fresh;     // [min(n * max_pages, n_pages)] (page, entry)
   int* old;        // [n * max_pages]: pages from `keep` on of a source compacted in place
 };
@@ -232,6 +277,7 @@ static size_t move_ws(const mv_cache_shape& s, int n, char* base, MoveWs* w) {
   MoveWs t;
   t.head = reinterpret_cast<int*>(put(16));
   t.rec = reinterpret_cast<MoveRec*>(put(sizeof(MoveRec) * n));
+  t.off = reinterpret_cast<int*>(put(sizeof(int) * n));
   t.fresh = reinterpret_cast<int2*>(put(sizeof(int2) * fresh));
   t.old = reinterpret_cast<int*>(put(sizeof(int) * tables));
   if (w) *w = t;
@@ -242,14 +288,35 @@ size_t cache_move_ws_bytes(const mv_cache_shape& s, int n) {
   return move_ws(s, n, nullptr, nullptr);
 }
 
-__device__ __forceinline__ int wave_sum(int x) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
+// Entry e's words, the lengths of its sequences and a span, as read
+struct MoveIn {
+  int src, dst, span0, span1, len, dst_len;
+  mv_span span;    // of lane `lane`
+  int prev;        // the end of the one before
+  __device__ __forceinline__ MoveIn(const CacheDev& a, const int32_t* s, const int32_t* d,
+                                    const int32_t* span_ptr, const mv_span* spans, int n_spans,
+                                    int e, int lane)
+      : src(s[e]), dst(d[e]), span0(span_ptr ? span_ptr[e] : 0),
+        span1(span_ptr ? span_ptr[e + 1] : 0) {
+    len = unsigned(src) < unsigned(a.n_seqs) ? a.length(src) : 0;
+    dst_len = unsigned(dst) < unsigned(a.n_seqs) ? a.len[dst] : 0;
+    read(spans, n_spans, lane);
+  }
+  __device__ __forceinline__ void read(const mv_span* spans, int n_spans, int lane) {
+    const int64_t j = int64_t(span0) + lane;
+    const bool in = j >= 0 && j < n_spans;
+    span = in ? spans[j] : mv_span{0, 0};
+    prev = in && lane > 0 ? spans[j - 1].end : 0;
+  }
+};
+
+// over groups of gs lanes (a power of two)
+__device__ __forceinline__ int group_sum(int x, int gs) {
+  for (int o = gs >> 1; o; o >>= 1) x += __shfl_xor(x, o);
   return x;
 }
-__device__ __forceinline__ int wave_min(int x) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) x = min(x, __shfl_xor(x, o));
+__device__ __forceinline__ int group_min(int x, int gs) {
+  for (int o = gs >> 1; o; o >>= 1) x = min(x, __shfl_xor(x, o));
   return x;
 }
 
@@ -264,11 +331,16 @@ __global__ __launch_bounds__(kPlan) void cache_plan_kernel(CacheDev a, int n,
   __shared__ uint32_t inplace[kMaxSeqs / 32];
   __shared__ int tmp[kPlan / 64 + 1];
   __shared__ int cnt[2], cut;
-  const int tid = threadIdx.x, lane = tid & 63;
+  const int tid = threadIdx.x;
+  // A wave to an entry, or a lane if there are no spans to read.  What the first
+  // entries read is asked for before anything waits.
+  const int gs = span_ptr ? 64 : 1, lane = tid & (gs - 1);
+  const MoveIn ahead(a, src, dst, span_ptr, spans, n_spans, min(tid / gs, n - 1), lane);   // (n >= 1)
+  const Search from(a);
   for (int s = tid; s < a.n_seqs; s += kPlan) claim[s] = n;
   for (int s = tid; s < kMaxSeqs / 32; s += kPlan) inplace[s] = 0;
   if (tid == 0) cnt[0] = cnt[1] = 0, cut = INT32_MAX;
-  __syncthreads();
+  lds_barrier();
   for (int e = tid; e < n; e += kPlan) {
     const int s = src[e], t = dst[e];
     if (unsigned(t) < unsigned(a.n_seqs)) {
@@ -276,38 +348,38 @@ __global__ __launch_bounds__(kPlan) void cache_plan_kernel(CacheDev a, int n,
       if (s == t && span_ptr) atomicOr(&inplace[t >> 5], 1u << (t & 31));
     }
   }
-  __syncthreads();
-  // a wave to an entry: its spans, and what becomes of its pages
+  lds_barrier();
+  // an entry's spans, and what becomes of its pages
   const int mask = (1 << a.psl) - 1;
-  for (int e = tid >> 6; e < n; e += kPlan / 64) {
+  for (int e = tid / gs; e < n; e += kPlan / gs) {
+    MoveIn in = e == tid / gs ? ahead : MoveIn(a, src, dst, span_ptr, spans, n_spans, e, lane);
     MoveRec r{};
-    r.src = src[e];
-    r.dst = dst[e];
+    r.src = in.src;
+    r.dst = in.dst;
     bool ok = unsigned(r.src) < unsigned(a.n_seqs) && unsigned(r.dst) < unsigned(a.n_seqs);
     ok = ok && claim[r.dst] == e;
     if (ok && r.src != r.dst)
-      ok = a.len[r.dst] == 0 && !(inplace[r.src >> 5] >> (r.src & 31) & 1);
+      ok = in.dst_len == 0 && !(inplace[r.src >> 5] >> (r.src & 31) & 1);
     if (!span_ptr) {
       ok = ok && r.src != r.dst;   // a fork
     } else {
-      r.span0 = span_ptr[e];
-      r.n_spans = span_ptr[e + 1] - r.span0;
+      r.span0 = in.span0;
+      r.n_spans = in.span1 - in.span0;
       ok = ok && r.span0 >= 0 && r.n_spans >= 0 && r.span0 <= n_spans - r.n_spans;
     }
-    if (ok) {
-      r.len = a.length(r.src);
+    if (ok) {   // (the same in every lane of the group)
+      r.len = in.len;
       int gone = 0, first = INT32_MAX, bad = 0;
-      for (int j = lane; j < r.n_spans; j += 64) {
-        const mv_span x = spans[r.span0 + j];
-        const int prev = j > 0 ? spans[r.span0 + j - 1].end : 0;
-        bad |= x.begin < prev || x.end < x.begin;
-        const int b = min(x.begin, r.len), t = min(x.end, r.len);
+      for (int j = lane; j < r.n_spans; j += gs) {
+        if (j != lane) in.read(spans, n_spans, j);
+        bad |= in.span.begin < in.prev || in.span.end < in.span.begin;
+        const int b = min(in.span.begin, r.len), t = min(in.span.end, r.len);
         gone += t - b;
         if (t > b) first = min(first, b);
       }
-      bad = wave_sum(bad);
-      gone = wave_sum(gone);
-      first = min(wave_min(first), r.len);
+      bad = group_sum(bad, gs);
+      gone = group_sum(gone, gs);
+      first = min(group_min(first, gs), r.len);
       ok = bad == 0;
       r.new_len = r.len - gone;
       r.old_pages = a.pages_of(r.len);
@@ -319,35 +391,37 @@ __global__ __launch_bounds__(kPlan) void cache_plan_kernel(CacheDev a, int n,
         r.keep += 1;
       r.n_new = a.pages_of(r.new_len) - r.keep;
       if (ok && r.src == r.dst)
-        for (int j = r.keep + lane; j < r.old_pages; j += 64)
+        for (int j = r.keep + lane; j < r.old_pages; j += gs)
           w.old[int64_t(e) * a.max_pages + j - r.keep] = a.page(r.src, j);
     }
     if (!ok) r.n_new = 0;
     r.ok = ok;
     if (lane == 0) {
       w.rec[e] = r;
+      pre[e] = r.n_new;
       if (!ok) atomicAdd(&cnt[1], 1);
     }
   }
-  __syncthreads();
+  lds_barrier();
   int need = 0;
   for (int e0 = 0; e0 < n; e0 += kPlan) {
     const int e = e0 + tid;
     int total;
-    const int before = need + block_scan<kPlan>(e < n ? w.rec[e].n_new : 0, tmp, total);
+    const int before = need + block_scan<kPlan>(e < n ? pre[e] : 0, tmp, total);
     if (e < n) {
       pre[e] = before;
-      w.rec[e].off = before;
+      w.off[e] = before;
     }
     need += total;   // at most the table's entries: destinations are named once
   }
   if (tid == 0) pre[n] = need;
-  __syncthreads();
-  const int found = deal_pages(a, need, tmp, [&](int q, int page) {
-    w.fresh[q] = make_int2(page, entry_of(pre, n, q));
+  lds_barrier();
+  const int found = deal_pages(a, pre, n, need, from, tmp, [&](int q, int e, int page) {
+    w.fresh[q] = make_int2(page, e);
     a.refs[page] = 1;
   });
   if (found < need) {
+    __syncthreads();   // what was dealt is read back
     for (int e = tid; e < n; e += kPlan) {
       if (pre[e + 1] > found && pre[e + 1] > pre[e]) {
         w.rec[e].ok = 0;
@@ -388,7 +462,8 @@ __global__ __launch_bounds__(256) void cache_move_kernel(CacheDev a, int n,
         row[j] = p;
         atomicAdd(&a.refs[p], 1);
       }
-    for (int j = tid; j < r.n_new; j += 256) row[r.keep + j] = w.fresh[r.off + j].x;
+    const int off = w.off[blockIdx.x];
+    for (int j = tid; j < r.n_new; j += 256) row[r.keep + j] = w.fresh[off + j].x;
     if (same) {
       const int* old = w.old + int64_t(blockIdx.x) * a.max_pages;
       int mine = INT32_MAX;
@@ -413,7 +488,7 @@ __global__ __launch_bounds__(256) void cache_move_kernel(CacheDev a, int n,
     const int q = int(x / a.n_layers), layer = int(x - int64_t(q) * a.n_layers);
     const int2 f = w.fresh[q];
     const MoveRec r = w.rec[f.y];
-    const int i0 = (r.keep + q - r.off) << a.psl;      // first new row of the page
+    const int i0 = (r.keep + q - w.off[f.y]) << a.psl;   // first new row of the page
     const int cnt = min(P, r.new_len - i0);
     __syncthreads();
     if (tid < cnt) {
@@ -431,23 +506,35 @@ __global__ __launch_bounds__(256) void cache_move_kernel(CacheDev a, int n,
       from[tid] = int64_t(p) * a.Hkv * hs + int64_t(at & (P - 1)) * a.D;
     }
     __syncthreads();
+    // a thread to a 16-byte chunk of a row, four heads' K and V at a time
     const int64_t to = int64_t(f.x) * a.Hkv * hs;
-    const u16* k = a.k + layer * ls;
-    const u16* v = a.v + layer * ls;
-    const int chunks = a.Hkv * cnt * CH;
-#pragma unroll 4
-    for (int y = tid; y < chunks; y += 256) {
-      const int c = y % CH, i = y / CH % cnt, h = y / CH / cnt;
-      const int64_t s = from[i] + h * hs + c * 8, t = to + h * hs + int64_t(i) * a.D + c * 8;
-      const uint4 kk = ld16(k + s), vv = ld16(v + s);
-      st16(a.k + layer * ls + t, kk);
-      st16(a.v + layer * ls + t, vv);
+    u16* k = a.k + layer * ls;
+    u16* v = a.v + layer * ls;
+    const int c = (tid & (CH - 1)) * 8;
+    for (int i = tid / CH; i < cnt; i += 256 / CH) {
+      const int64_t s = from[i] + c, t = to + int64_t(i) * a.D + c;
+      for (int h = 0; h < a.Hkv; h += 4) {
+        uint4 kk[4], vv[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          if (h + x < a.Hkv) {
+            kk[x] = ld16(k + s + (h + x) * hs);
+            vv[x] = ld16(v + s + (h + x) * hs);
+          }
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          if (h + x < a.Hkv) {
+            st16(k + t + (h + x) * hs, kk[x]);
+            st16(v + t + (h + x) * hs, vv[x]);
+          }
+      }
     }
   }
 }
 
-// A block to an entry.
-__global__ __launch_bounds__(256) void cache_free_kernel(CacheDev a, int n,
+// A block to an entry, of many threads: a page is a chain of a table entry and
+// an atomic that returns, 1250 of them took 9.6 us by 256 threads.
+__global__ __launch_bounds__(kPlan) void cache_free_kernel(CacheDev a, int n,
                                                          const int32_t* __restrict__ ids) {
   __shared__ int low, seen;
   const int e = blockIdx.x, tid = threadIdx.x, s = ids[e];
@@ -457,7 +544,7 @@ __global__ __launch_bounds__(256) void cache_free_kernel(CacheDev a, int n,
   }
   if (tid == 0) low = INT32_MAX, seen = 0;
   __syncthreads();
-  for (int j = tid; j < e; j += 256)
+  for (int j = tid; j < e; j += kPlan)
     if (ids[j] == s) seen = 1;
   __syncthreads();
   if (seen) return;   // an earlier entry frees it
@@ -465,7 +552,7 @@ __global__ __launch_bounds__(256) void cache_free_kernel(CacheDev a, int n,
   __syncthreads();    // the length is read before it is cleared
   int32_t* row = a.table + int64_t(s) * a.max_pages;
   int mine = INT32_MAX;
-  for (int j = tid; j < pages; j += 256) {
+  for (int j = tid; j < pages; j += kPlan) {
     const int p = a.page(s, j);
     row[j] = -1;
     if (atomicSub(&a.refs[p], 1) == 1) mine = min(mine, p);
@@ -529,7 +616,7 @@ hipError_t launch_cache_move(const mv_cache_shape& shape, const CacheDev& a, int
 
 hipError_t launch_cache_free(const CacheDev& a, int n, const int32_t* ids, hipStream_t stream) {
   ProfScope prof("cache_free", stream);
-  hipLaunchKernelGGL(cache_free_kernel, dim3(n), dim3(256), 0, stream, a, n, ids);
+  hipLaunchKernelGGL(cache_free_kernel, dim3(n), dim3(kPlan), 0, stream, a, n, ids);
   return hipGetLastError();
 }
 

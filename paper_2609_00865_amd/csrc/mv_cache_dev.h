@@ -33,20 +33,36 @@ struct CacheDev {
 // ctl words
 enum { kCtlHint = 0, kCtlNoPages = 1, kCtlBad = 2, kCtlFree = 3 };
 
+// A barrier that orders LDS alone.  __syncthreads also waits for every global
+// store of the block to arrive, about a microsecond each time.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// Inclusive prefix sum over the wave by data-parallel moves between lanes (six
+// vector instructions; through LDS the same six steps take ten times as long).
+__device__ __forceinline__ int wave_scan(int x) {
+  constexpr int kShr = 0x110, kBcast15 = 0x142, kBcast31 = 0x143;
+  x += __builtin_amdgcn_update_dpp(0, x, kShr + 1, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, kShr + 2, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, kShr + 4, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, kShr + 8, 0xf, 0xf, false);   // rows of 16
+  x += __builtin_amdgcn_update_dpp(0, x, kBcast15, 0xa, 0xf, false);   // rows 0 -> 1, 2 -> 3
+  x += __builtin_amdgcn_update_dpp(0, x, kBcast31, 0xc, 0xf, false);   // rows 0, 1 -> 2, 3
+  return x;
+}
+
 // Exclusive prefix sum of v over the block (BLOCK threads) and the total;
 // tmp: BLOCK / 64 + 1 ints of LDS.
 template <int BLOCK>
 __device__ __forceinline__ int block_scan(int v, int* tmp, int& total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int x = v;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(x, o);
-    if (lane >= o) x += y;
-  }
-  __syncthreads();   // tmp of an earlier call is read
+  const int x = wave_scan(v);
+  lds_barrier();   // tmp of an earlier call is read
   if (lane == 63) tmp[wave] = x;
-  __syncthreads();
+  lds_barrier();
   int before = 0, all = 0;
 #pragma unroll
   for (int w = 0; w < BLOCK / 64; ++w) {

@@ -33,7 +33,7 @@ struct TreeArgs {
   float* lse;
   float* part_o;       // [2 * groups][R][D] unnormalised
   float* part_ml;      // [2 * groups][R][2] maximum (base 2, scaled), sum
-  struct TreeJoin* join;   // [groups]
+  struct TreeJoin* join;   // [tiles][Hkv]
   const int32_t* table;
   const int32_t* len;
   const int32_t* ids;
@@ -46,12 +46,12 @@ struct TreeArgs {
   float scale_log2;
 };
 
-// What is to be joined of the tile that begins in workgroup g's run and goes on
-// in the next ones': its first segment is at `slot`, run g + j's at 2 (g + j).
+// What is to be joined of a tile place and KV head: the tile's first segment,
+// of run `run`, is at `slot`, that of run r > run at 2 r.
 struct TreeJoin {
-  int rows;            // pairs of the tile; 0: nothing begins in g and goes on
-  int m0, r0, hk;      // first pair, the entry's first row of q, KV head
-  int runs, slot;
+  int rows;            // pairs of the tile; 0: no tile, or it was written whole
+  int m0, r0;          // first pair, the entry's first row of q
+  int run, slot, runs;
   int pad[2];
 };
 
@@ -152,8 +152,11 @@ __device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {   // of what
 
 // The deal: every workgroup works out the same one from the lengths, and
 // walks its own run of it, segment by segment.
-template <int R, int BLOCK>
+// AGAIN: the arguments are read from where they were passed each time (the
+// kernel has no scalar registers to hold them in).
+template <int R, int BLOCK, bool AGAIN>
 struct Deal {
+  const TreeArgs& direct;
   TreeShared& s;
   int64_t units;       // of one KV head
   int64_t per;         // of a run
@@ -165,20 +168,27 @@ struct Deal {
   int hk, unit, n, of;
   int run;
 
+  __device__ __forceinline__ const TreeArgs& args() const {
+    if constexpr (AGAIN) return again();
+    return direct;
+  }
+
   // The units of places [j BLOCK, (j + 1) BLOCK) and before each of them.
   __device__ __forceinline__ void scan(int j, Tile& mine, int& before, int& total) {
-    const TreeArgs& a = again();
+    const TreeArgs& a = args();
     const int u = j * BLOCK + threadIdx.x;
     mine = Tile{};
     if (u < a.tiles) mine = tile_of<R>(a, s, u);
+    if (blockIdx.x == 0 && u < a.tiles && mine.rows == 0)   // no run comes by here
+      for (int h = 0; h < a.Hkv; ++h) a.join[int64_t(u) * a.Hkv + h].rows = 0;
     // (a tile has fewer than 2^25 units: BLOCK of them do not pass 2^31 unless
     // the caches are past any memory, in which case the rows are unspecified)
     before = block_scan<BLOCK>(mine.units(), s.tmp, total);
   }
 
-  __device__ __forceinline__ Deal(TreeShared& sh, int r) : s(sh), run(r) {
-    const TreeArgs& a = again();
-    if (threadIdx.x == 0) a.join[run].rows = 0;
+  __device__ __forceinline__ Deal(const TreeArgs& a0, TreeShared& sh, int r)
+      : direct(a0), s(sh), run(r) {
+    const TreeArgs& a = args();
     if (a.B <= kPlanB) {
       for (int b = threadIdx.x; b <= a.B; b += BLOCK) {
         s.ptr[b] = min(max(a.ptr[b], 0), a.N);
@@ -235,7 +245,7 @@ struct Deal {
   __device__ __forceinline__ void next() {
     p += n;
     if (p >= end) return;
-    const TreeArgs& a = again();
+    const TreeArgs& a = args();
     int b = t.b, m0 = t.m0 + R;
     if (m0 >= t.n * a.G) {
       m0 = 0;
@@ -260,22 +270,26 @@ struct Deal {
   __device__ __forceinline__ int64_t slot() const { return 2 * int64_t(run) + (p != begin); }
 
   __device__ __forceinline__ const int32_t* pages() const {   // the sequence's row of the table
-    const TreeArgs& a = again();
+    const TreeArgs& a = args();
     const int id = uniform(a.B <= kPlanB ? s.id[t.b] : a.ids[t.b]);
     return a.table + int64_t(id) * a.max_pages;
   }
 
-  // For the join: the segment that a tile's other segments follow
+  // For the join: by the segment that a tile begins with
   __device__ __forceinline__ void note() const {
-    if (unit != 0 || whole() || threadIdx.x != 0) return;
+    if (unit != 0 || threadIdx.x != 0) return;
+    const TreeArgs& a = args();
+    const int place = first_place<R>(t.r0, t.b, a.G) + t.m0 / R;
     TreeJoin j{};
-    j.rows = t.rows;
-    j.m0 = t.m0;
-    j.r0 = t.r0;
-    j.hk = hk;
-    j.runs = int(quotient(p + of - 1, per)) - run + 1;
-    j.slot = int(slot());
-    again().join[run] = j;
+    if (!whole()) {
+      j.rows = t.rows;
+      j.m0 = t.m0;
+      j.r0 = t.r0;
+      j.run = run;
+      j.slot = int(slot());
+      j.runs = int(quotient(p + of - 1, per)) - run + 1;
+    }
+    a.join[int64_t(place) * a.Hkv + hk] = j;
   }
 };
 
@@ -432,7 +446,7 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
   __shared__ float sm[NW][R], sl[NW][R];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int c = lane & 31, g = lane >> 5;
-  Deal<R, BLOCK> deal(sh, run_of_block(a.groups));
+  Deal<R, BLOCK, false> deal(a, sh, run_of_block(a.groups));
   const int ps = 1 << a.psl;
   // A load's LR rows lie in one page; its address is scalar but for one of
   // 16 / LR offsets per lane (the chunks' permutation has a period of 16 rows).
@@ -487,13 +501,18 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
       const int key0 = key_of(x);
       pages.ahead(key0 >> a.psl, last);
       const uint32_t kl = lds0 + uint32_t(x & 1) * TB;
+      // (16 rows of a page at a time: the look-ups of a tile wait together)
+      int64_t at[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int key = key0 + j * 16;
+        at[j] = pages.get(min(key, last) >> a.psl) * page_bytes + (key & (ps - 1)) * (D * 2);
+      }
 #pragma unroll
       for (int j = 0; j < NI; ++j) {
-        const int key = key0 + j * LR;
-        const int64_t at = pages.get(min(key, last) >> a.psl) * page_bytes +
-                           (key & (ps - 1)) * (D * 2);
-        lds_load16s(kb + at, voff[j % NO], kl + j * 1024);
-        lds_load16s(vb + at, voff[j % NO], kl + 2 * TB + j * 1024);
+        const int64_t x0 = at[j / NO] + (j % NO) * 1024;
+        lds_load16s(kb + x0, voff[j % NO], kl + j * 1024);
+        lds_load16s(vb + x0, voff[j % NO], kl + 2 * TB + j * 1024);
       }
     };
     if (todo > 0) issue(0);
@@ -651,7 +670,7 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
   __shared__ TreeShared sh;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int c = lane & 31, g = lane >> 5;
-  Deal<R, BLOCK> deal(sh, run_of_block(a.groups));
+  Deal<R, BLOCK, true> deal(a, sh, run_of_block(a.groups));
   const int ps = 1 << a.psl;
   // A load's LR rows lie in one page (pages hold multiples of 16 rows), and
   // their chunks' permutation does not depend on which load of the tile it is:
@@ -972,15 +991,17 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
 }
 
 // --------------------------------------------------------------------------
-// Joins the segments of a tile, in their order: block (run, RG pairs), JG
+// Joins the segments of a tile, in their order: block (tile place, KV head,
+// RG pairs), JG
 // groups of D / 8 threads to a pair, each for every JG-th segment.
 // --------------------------------------------------------------------------
 template <int D, int R, int JG>
 __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
   constexpr int TD = D / 8, RG = 256 / (TD * JG), NG = R / RG, U = 4;
   __shared__ float so[JG][RG][D], sml[JG][RG][2];
-  const int run = blockIdx.x / NG, rg = blockIdx.x % NG;
-  const TreeJoin jn = a.join[run];
+  const int rg = blockIdx.x % NG;
+  const TreeJoin jn = a.join[blockIdx.x / NG];
+  const int hk = blockIdx.x / NG % a.Hkv;
   if (rg * RG >= jn.rows) return;   // block-uniform
   const int d0 = (threadIdx.x % TD) * 8, rr = threadIdx.x / TD % RG, jg = threadIdx.x / (TD * RG);
   const int r = rg * RG + rr;
@@ -992,7 +1013,7 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
 #pragma unroll
       for (int x = 0; x < U; ++x) {
         const int j = min(j0 + x * JG, jn.runs - 1);
-        const int64_t s = int64_t(j == 0 ? jn.slot : 2 * (run + j)) * R + r;
+        const int64_t s = int64_t(j == 0 ? jn.slot : 2 * (jn.run + j)) * R + r;
         ml[x] = *reinterpret_cast<const float2*>(a.part_ml + 2 * s);
         oj[x][0] = *reinterpret_cast<const float4*>(a.part_o + s * D + d0);
         oj[x][1] = *reinterpret_cast<const float4*>(a.part_o + s * D + d0 + 4);
@@ -1043,7 +1064,7 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
   if (r >= jn.rows) return;
   Tile t{};
   t.r0 = jn.r0;
-  const Pair pr(a, t, jn.hk, jn.m0 + r);
+  const Pair pr(a, t, hk, jn.m0 + r);
   const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
   for (int e = 0; e < 8; ++e) y[e] *= inv;
@@ -1118,7 +1139,7 @@ static TreePlan tree_plan(const mv_cache_shape& c, const mv_tree_attn_shape& s) 
   p.groups = tree_groups(c, s, p.tiles);
   p.o_bytes = size_t(2 * p.groups) * p.R * c.head_dim * 4;
   p.ml_bytes = size_t(2 * p.groups) * p.R * 2 * 4;
-  p.bytes = p.o_bytes + p.ml_bytes + sizeof(TreeJoin) * p.groups;
+  p.bytes = p.o_bytes + p.ml_bytes + sizeof(TreeJoin) * p.tiles * c.n_heads_kv;
   return p;
 }
 
@@ -1126,8 +1147,9 @@ static TreePlan tree_plan(const mv_cache_shape& c, const mv_tree_attn_shape& s) 
 // takes depends on both.
 size_t tree_attn_ws_bytes(const mv_cache_shape& c, const mv_tree_attn_shape& s) {
   const int G = s.n_heads_q / c.n_heads_kv;
-  const int64_t groups = tree_groups(c, s, int64_t(s.n_rows) * G / 32 + s.n_batch);
-  return size_t(2 * groups) * 128 * (c.head_dim + 2) * 4 + sizeof(TreeJoin) * groups;
+  const int64_t tiles = int64_t(s.n_rows) * G / 32 + s.n_batch;
+  return size_t(2 * tree_groups(c, s, tiles)) * 128 * (c.head_dim + 2) * 4 +
+         sizeof(TreeJoin) * size_t(tiles) * c.n_heads_kv;
 }
 
 // Tile places past which the deal does not fit its LDS
@@ -1150,17 +1172,23 @@ static hipError_t launch_tree(const TreePlan& p, TreeArgs a, hipStream_t stream)
   // one workgroup's run is every tile
   if (p.groups == 1) return hipSuccess;
   ProfScope prof("tree_combine", stream);
-  // Tiles of many segments are joined by four groups of threads a pair, each
-  // with every fourth one; where there are few to a tile, blocks of four times
-  // the pairs (a quarter of the blocks) do it sooner.
-  const bool wide = p.groups >= 8 * int64_t(p.tiles) * a.Hkv;
-#define MV_JOIN(R, JG)                                                                        \
-  hipLaunchKernelGGL((tree_join_kernel<D, R, JG>), dim3(unsigned(p.groups * (R * JG * D / 2048))), \
-                     dim3(256), 0, stream, a)
-  if (p.many && wide) MV_JOIN(128, 4);
-  else if (p.many) MV_JOIN(128, 1);
-  else if (wide) MV_JOIN(32, 4);
-  else MV_JOIN(32, 1);
+  // The more segments a tile may have, the more groups of threads share a pair's
+  // (one sequence of 8000 keys, 125 segments a tile: 15 us by four groups, less
+  // by sixteen); where there are few, blocks of more pairs do it sooner.
+  const int64_t segments = p.groups / (int64_t(p.tiles) * a.Hkv);
+#define MV_JOIN(R, JG)                                                                         \
+  hipLaunchKernelGGL((tree_join_kernel<D, R, JG>),                                             \
+                     dim3(unsigned(p.tiles * a.Hkv * (R * JG * D / 2048))), dim3(256), 0, stream, \
+                     a)
+  if (p.many) {
+    if (segments >= 32) MV_JOIN(128, 16);
+    else if (segments >= 8) MV_JOIN(128, 4);
+    else MV_JOIN(128, 1);
+  } else {
+    if (segments >= 32) MV_JOIN(32, 16);
+    else if (segments >= 8) MV_JOIN(32, 4);
+    else MV_JOIN(32, 1);
+  }
 #undef MV_JOIN
   return hipGetLastError();
 }

@@ -107,6 +107,7 @@ def test_padding_duplicates_and_bad_ids():
     p.reserve([2, -1, 2, 9, -3], [0, 3, 7, 9, 10, 12])        # padded rows, a repeat, bad ids
     p.reserve([1, 3], [2, 5, 5], n_new=8)                     # rows no entry covers
     p.reserve([1, 3, 0], [0, 4, 2, 6], n_new=5)               # falling, and past n_new
+    p.reserve([], [0], n_new=3)                               # no entry at all
     p.status()
     p.free([2, 2, -1, 8, -5, 4])
     p.status()
