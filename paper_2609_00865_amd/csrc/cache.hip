@@ -15,6 +15,7 @@ namespace mv {
 
 constexpr int kPlan = 1024;   // threads of the planning blocks
 constexpr int kMaxSeqs = MV_CACHE_MAX_SEQS;
+constexpr int kTogether = 16;  // entries up to which a plan's threads share each one's pages
 
 __global__ __launch_bounds__(256) void cache_reset_kernel(CacheDev a) {
   const int64_t n = int64_t(a.n_seqs) * a.max_pages;
@@ -329,6 +330,7 @@ __global__ __launch_bounds__(kPlan) void cache_plan_kernel(CacheDev a, int n,
   __shared__ int claim[kMaxSeqs];
   __shared__ int pre[kMaxSeqs + 1];
   __shared__ uint32_t inplace[kMaxSeqs / 32];
+  __shared__ int2 old_of[kTogether];   // first and past the last page a source in place may lose
   __shared__ int tmp[kPlan / 64 + 1];
   __shared__ int cnt[2], cut;
   const int tid = threadIdx.x;
@@ -390,7 +392,7 @@ __global__ __launch_bounds__(kPlan) void cache_plan_kernel(CacheDev a, int n,
           a.refs[a.page(r.src, r.keep)] == 1)
         r.keep += 1;
       r.n_new = a.pages_of(r.new_len) - r.keep;
-      if (ok && r.src == r.dst)
+      if (ok && r.src == r.dst && n > kTogether)
         for (int j = r.keep + lane; j < r.old_pages; j += gs)
           w.old[int64_t(e) * a.max_pages + j - r.keep] = a.page(r.src, j);
     }
@@ -400,9 +402,16 @@ __global__ __launch_bounds__(kPlan) void cache_plan_kernel(CacheDev a, int n,
       w.rec[e] = r;
       pre[e] = r.n_new;
       if (!ok) atomicAdd(&cnt[1], 1);
+      if (n <= kTogether) old_of[e] = make_int2(r.keep, ok && r.src == r.dst ? r.old_pages : 0);
     }
   }
   lds_barrier();
+  // The pages that sequences compacted in place are about to lose, all threads
+  // on one sequence if there are few (32768 rows in pages of 16: 6 us by a wave)
+  for (int e = 0; e < min(n, kTogether); ++e)
+    if (n <= kTogether)
+      for (int j = old_of[e].x + tid; j < old_of[e].y; j += kPlan)
+        w.old[int64_t(e) * a.max_pages + j - old_of[e].x] = a.page(src[e], j);
   int need = 0;
   for (int e0 = 0; e0 < n; e0 += kPlan) {
     const int e = e0 + tid;

@@ -308,6 +308,12 @@ __device__ __forceinline__ float weight(float m, float M) {
   return m == -INFINITY ? 1.f : fast_exp2(m - M);
 }
 
+// lse from a maximum (base 2) and the sum beside it, in 64 bits: once a row, and
+// the fp32 logarithm alone would be off by as much as all before it.
+__device__ __forceinline__ float lse_of(float M, float l) {
+  return l == 0.f ? -INFINITY : float(double(M) * 0.6931471805599453 + log(double(l)));
+}
+
 // The keys of [key0, key0 + 32) that new row i of a tile's entry sees, as
 // bits; row: its row of q.
 __device__ __forceinline__ uint32_t seen32(const TreeArgs& a, const Tile& t, int64_t row, int i,
@@ -556,11 +562,13 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
       const float mu = m_run == -INFINITY ? 0.f : m_run;
       // P in bf16 for the product (its sum is taken before the rounding): half
       // an ulp of each, 2^-8 relative, averaged over the row
+      float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         sc[r] = fast_exp2(fmaf(sc[r], a.scale_log2, -mu));
-        l_run += sc[r];
+        part[r & 3] += sc[r];
       }
+      l_run += (part[0] + part[1]) + (part[2] + part[3]);
       if (masked) {
         // A value that is not finite in a row that some query does not see
         // would reach it as 0 * inf: such elements are taken out of the tile
@@ -637,8 +645,7 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
         for (int e = 0; e < 8; ++e) y[e] *= inv;
         store_v<8>(a.o + (pr.row * a.Hq + pr.h) * D + d0, y);
         if (d0 == 0)
-          a.lse[int64_t(pr.h) * a.N + pr.row] =
-              l == 0.f ? -INFINITY : (Mr + __log2f(l)) * 0.69314718055994531f;
+          a.lse[int64_t(pr.h) * a.N + pr.row] = lse_of(Mr, l);
       } else {
         float* q = a.part_o + (slot * R + r) * D + d0;
         *reinterpret_cast<float4*>(q) = make_float4(y[0], y[1], y[2], y[3]);
@@ -967,8 +974,7 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
                 make_uint2(pack2(oacc[db][q4 * 4 + 0] * inv, oacc[db][q4 * 4 + 1] * inv),
                            pack2(oacc[db][q4 * 4 + 2] * inv, oacc[db][q4 * 4 + 3] * inv));
         if (g == 0)
-          b.lse[int64_t(mine.h) * b.N + mine.row] =
-              l == 0.f ? -INFINITY : (m_run + __log2f(l)) * 0.69314718055994531f;
+          b.lse[int64_t(mine.h) * b.N + mine.row] = lse_of(m_run, l);
       } else {
         const int64_t s = deal.slot() * R + my;
         float* op = b.part_o + s * D;
@@ -1070,8 +1076,7 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
   for (int e = 0; e < 8; ++e) y[e] *= inv;
   store_v<8>(a.o + (pr.row * a.Hq + pr.h) * D + d0, y);
   if (d0 == 0)
-    a.lse[int64_t(pr.h) * a.N + pr.row] =
-        l == 0.f ? -INFINITY : (M + __log2f(l)) * 0.69314718055994531f;
+    a.lse[int64_t(pr.h) * a.N + pr.row] = lse_of(M, l);
 }
 
 // A thread to a row: up the parents, its words from the highest down.
