@@ -75,9 +75,9 @@ struct TreeShared {
   int ptr[kPlanB + 1];
   int id[kPlanB], len[kPlanB];
   int tmp[17];
-  int64_t first[kChunks + 1];   // first unit of each BLOCK of places
+  int64_t units[kChunks], tiles[kChunks];   // before each BLOCK of places
   Tile tile;                    // where a run begins
-  int unit;
+  int at;
 };
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -151,30 +151,37 @@ __device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {   // of what
 }
 
 // The deal: every workgroup works out the same one from the lengths, and
-// walks its own run of it, segment by segment.
+// walks its own run of it, segment by segment.  To begin and end a tile takes
+// about as long as two units (the first keys' way from memory, the result's
+// way back), so where runs are long a tile counts for that many more: without
+// it, 4000 rows of a prompt over no context took 234 us, runs of many short
+// tiles being the last to end, and 64 rollouts' decode 111.
 // AGAIN: the arguments are read from where they were passed each time (the
 // kernel has no scalar registers to hold them in).
+constexpr int kTileCost = 2, kLongRun = 8;
+
 template <int R, int BLOCK, bool AGAIN>
 struct Deal {
   const TreeArgs& direct;
   TreeShared& s;
-  int64_t units;       // of one KV head
+  int extra;           // what a tile counts for beside its units
+  int64_t total;       // of one KV head: units and extras
   int64_t per;         // of a run
   int64_t begin, end;  // this run, over all KV heads
-  // the segment: its first unit among all, tile, KV head, first unit of the
-  // tile, units of the segment and of the tile
-  int64_t p;
+  // the segment: where it begins among all and what it counts for; its tile and
+  // KV head, where the tile begins, first unit, units of the segment and the tile
+  int64_t p, tile_p;
   Tile t;
-  int hk, unit, n, of;
-  int run;
+  int len, hk, unit, n, of;
+  int run, seg;
 
   __device__ __forceinline__ const TreeArgs& args() const {
     if constexpr (AGAIN) return again();
     return direct;
   }
 
-  // The units of places [j BLOCK, (j + 1) BLOCK) and before each of them.
-  __device__ __forceinline__ void scan(int j, Tile& mine, int& before, int& total) {
+  // The tiles of places [j BLOCK, (j + 1) BLOCK): units and tiles before each
+  __device__ __forceinline__ void scan(int j, Tile& mine, int (&before)[2], int (&sum)[2]) {
     const TreeArgs& a = args();
     const int u = j * BLOCK + threadIdx.x;
     mine = Tile{};
@@ -183,11 +190,12 @@ struct Deal {
       for (int h = 0; h < a.Hkv; ++h) a.join[int64_t(u) * a.Hkv + h].rows = 0;
     // (a tile has fewer than 2^25 units: BLOCK of them do not pass 2^31 unless
     // the caches are past any memory, in which case the rows are unspecified)
-    before = block_scan<BLOCK>(mine.units(), s.tmp, total);
+    before[0] = block_scan<BLOCK>(mine.units(), s.tmp, sum[0]);
+    before[1] = block_scan<BLOCK>(mine.rows > 0, s.tmp, sum[1]);
   }
 
   __device__ __forceinline__ Deal(const TreeArgs& a0, TreeShared& sh, int r)
-      : direct(a0), s(sh), run(r) {
+      : direct(a0), s(sh), run(r), seg(0) {
     const TreeArgs& a = args();
     if (a.B <= kPlanB) {
       for (int b = threadIdx.x; b <= a.B; b += BLOCK) {
@@ -201,49 +209,66 @@ struct Deal {
     __syncthreads();
     const int chunks = (a.tiles + BLOCK - 1) / BLOCK;
     Tile mine;
-    int before = 0, total;
-    int64_t sum = 0;
+    int before[2] = {0, 0}, sum[2];
+    int64_t units = 0, tiles = 0;
     for (int j = 0; j < chunks; ++j) {
-      scan(j, mine, before, total);
-      if (threadIdx.x == 0) s.first[j] = sum;
-      sum += total;
+      scan(j, mine, before, sum);
+      if (threadIdx.x == 0) {
+        s.units[j] = units;
+        s.tiles[j] = tiles;
+      }
+      units += sum[0];
+      tiles += sum[1];
     }
-    units = uniform(sum);
-    per = max(int64_t(1), quotient(units * a.Hkv + a.groups - 1, a.groups));
+    units = uniform(units);
+    tiles = uniform(tiles);
+    extra = units * a.Hkv >= int64_t(kLongRun) * a.groups ? kTileCost : 0;
+    total = units + extra * tiles;
+    per = max(int64_t(1), quotient(total * a.Hkv + a.groups - 1, a.groups));
     begin = run * per;
-    end = min(begin + per, units * a.Hkv);
+    end = min(begin + per, total * a.Hkv);
     p = begin;
     if (p >= end) return;
-    hk = uniform(int(quotient(p, units)));
-    int64_t x = p - hk * units;
+    hk = uniform(int(quotient(p, total)));
+    int64_t x = p - hk * total;
     if (chunks > 1) {
-      __syncthreads();
+      lds_barrier();
       int lo = 0, hi = chunks;
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (s.first[mid] <= x) lo = mid; else hi = mid;
+        if (s.units[mid] + extra * s.tiles[mid] <= x) lo = mid; else hi = mid;
       }
       lo = uniform(lo);
-      x -= s.first[lo];
-      scan(lo, mine, before, total);
+      x -= s.units[lo] + extra * s.tiles[lo];
+      scan(lo, mine, before, sum);
     }
-    if (x >= before && x < before + mine.units()) {
+    const int first = before[0] + extra * before[1];
+    if (mine.rows > 0 && x >= first && x < first + mine.units() + extra) {
       s.tile = mine;
-      s.unit = int(x) - before;
+      s.at = int(x) - first;
     }
-    __syncthreads();
+    lds_barrier();
     t = uniform(s.tile);
-    unit = uniform(s.unit);
+    enter(uniform(s.at));
+    if (n == 0) next();
+  }
+
+  // the run's part of the tile from place `at` of it on
+  __device__ __forceinline__ void enter(int at) {
     of = t.units();
-    n = int(min(int64_t(of - unit), end - p));
+    tile_p = p - at;
+    len = int(min(int64_t(of + extra - at), end - p));
+    unit = max(0, at - extra);
+    n = max(0, at + len - extra) - unit;
   }
 
   __device__ __forceinline__ bool done() const { return p >= end; }
 
   // On to the next tile: of the entry, of the next entry that has rows, of the
-  // next KV head.
+  // next KV head.  (A run that ends before a tile's first unit leaves it.)
   __device__ __forceinline__ void next() {
-    p += n;
+    if (n > 0) ++seg;
+    p += len;
     if (p >= end) return;
     const TreeArgs& a = args();
     int b = t.b, m0 = t.m0 + R;
@@ -260,14 +285,13 @@ struct Deal {
       } while (uniform(first_row(a, s, b + 1)) <= uniform(first_row(a, s, b)));
     }
     t = uniform(tile_at<R>(a, s, b, m0));
-    unit = 0;
-    of = t.units();
-    n = int(min(int64_t(of), end - p));
+    enter(0);
+    if (n == 0) p = end;
   }
 
   __device__ __forceinline__ bool whole() const { return n == of; }
   // where the segment's partial result goes
-  __device__ __forceinline__ int64_t slot() const { return 2 * int64_t(run) + (p != begin); }
+  __device__ __forceinline__ int64_t slot() const { return 2 * int64_t(run) + (seg != 0); }
 
   __device__ __forceinline__ const int32_t* pages() const {   // the sequence's row of the table
     const TreeArgs& a = args();
@@ -287,7 +311,7 @@ struct Deal {
       j.r0 = t.r0;
       j.run = run;
       j.slot = int(slot());
-      j.runs = int(quotient(p + of - 1, per)) - run + 1;
+      j.runs = int(quotient(tile_p + extra + of - 1, per)) - run + 1;
     }
     a.join[int64_t(place) * a.Hkv + hk] = j;
   }
@@ -662,17 +686,20 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
 }
 
 // --------------------------------------------------------------------------
-// many pairs: four waves of 32 pairs on shared 64-key tiles
+// many pairs: four waves of 32 pairs on shared tiles of 32 KB keys, K and V in
+// NB buffers each
 // --------------------------------------------------------------------------
-template <int D>
+template <int D, int KB, int NB>
 __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
-  constexpr int R = 128, BK = 64, BLOCK = 256;
+  constexpr int R = 128, BK = 32 * KB, BLOCK = 256;
   constexpr int KS = D / 16, DB = D / 32;
   constexpr int TB = BK * D * 2;             // bytes of a tile
   constexpr int NL = TB / 4096;              // loads of a thread per tile
   constexpr int LR = 512 / D;                // rows of a wave's load
-  __shared__ __align__(1024) char sKb[2][TB];
-  __shared__ __align__(1024) char sVb[2][TB];
+  constexpr int H = 8 * KB;                  // half the elements of a tile in a lane
+  static_assert(NB % 2 == 0, "score sets take turns with the buffers");
+  __shared__ __align__(1024) char sKb[NB][TB];
+  __shared__ __align__(1024) char sVb[NB][TB];
   __shared__ __align__(16) int pg[4][128];
   __shared__ TreeShared sh;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
@@ -688,7 +715,7 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
 
   for (; !deal.done(); deal.next()) {
     const Tile& t = deal.t;
-    const int hk = deal.hk, n = deal.n;   // n: 64-key tiles of the segment
+    const int hk = deal.hk;
 
     const int my = wave * 32 + c;
     const bool qok = my < t.rows;
@@ -716,8 +743,11 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
       for (int r = 0; r < 16; ++r) oacc[db][r] = 0.f;
     float m_run = -INFINITY, l_run = 0.f;
 
-    const int key_base = deal.unit * BK;
+    const int key_base = deal.unit * kUnit;
     const int last = t.kmax - 1;
+    // tiles of the segment
+    const int n = (int(min(int64_t(t.kmax), int64_t(deal.unit + deal.n) * kUnit)) - key_base +
+                   BK - 1) / BK;
     const uint32_t page_rows = uint32_t(a.Hkv) * ps;   // (a pool of 2^32 rows is past any memory)
     const char* kb = reinterpret_cast<const char*>(a.k) + int64_t(hk) * ps * D * 2;
     const char* vb = reinterpret_cast<const char*>(a.v) + int64_t(hk) * ps * D * 2;
@@ -745,7 +775,7 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
     };
     uint32_t at_v[NL], at_k[NL];   // of the V tile and of the K tile to be asked for next
     auto kfrag = [&](int buf, int j) {
-      return ld_row_swz<D>(&sKb[buf][0], (j & 1) * 32 + c, (j >> 1) * 2 + g);
+      return ld_row_swz<D>(&sKb[buf][0], (j % KB) * 32 + c, (j / KB) * 2 + g);
     };
     const int clear = a.tree ? t.c : t.c + t.m0 / a.G + 1;   // keys every row of the tile sees
     auto masked = [&](int x) { return key_base + x * BK + BK > min(clear, t.kmax); };
@@ -756,21 +786,21 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
       const Pair mine = pair(b);
       return seen32(b, t, mine.row, mine.i, key0) & in;
     };
-    f32x16 sc[2][2];   // scores of tile x in sc[x & 1]
-    auto mask_tile = [&](f32x16 (&s)[2], int x) {
+    f32x16 sc[2][KB];   // scores of tile x in sc[x & 1]
+    auto mask_tile = [&](f32x16 (&s)[KB], int x) {
       if (!masked(x)) return;   // block-uniform
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
+      for (int b = 0; b < KB; ++b) {
         const uint32_t w = seen(x, b) >> (g * 4);
 #pragma unroll
         for (int r = 0; r < 16; ++r)
           s[b][r] = (w >> ((r >> 2) * 8 + (r & 3))) & 1u ? s[b][r] : -INFINITY;
       }
     };
-    auto tile_max = [&](const f32x16 (&s)[2]) {
+    auto tile_max = [&](const f32x16 (&s)[KB]) {
       float mx = -INFINITY;
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+      for (int b = 0; b < KB; ++b)
 #pragma unroll
         for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[b][r]);
       return max_halves(mx) * a.scale_log2;
@@ -779,14 +809,14 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
     // a tile that the row has scored before; only where they would pass 2^16,
     // or a row has seen no key yet, is the tile's own maximum taken.
     auto m_off = [&]() { return m_run == -INFINITY ? 0.f : m_run; };
-    auto pexp = [&](const f32x16 (&s)[2], int i, float mu) {
+    auto pexp = [&](const f32x16 (&s)[KB], int i, float mu) {
       return fast_exp2(fmaf(s[i >> 4][i & 15], a.scale_log2, -mu));
     };
     auto pack8 = [](const float* q) {
       return as_bf16x8(make_uint4(pack2(q[0], q[1]), pack2(q[2], q[3]), pack2(q[4], q[5]),
                                   pack2(q[6], q[7])));
     };
-    auto slow_tile = [&](const f32x16 (&s)[2], bf16x8 (&pf)[4], float& psum)
+    auto slow_tile = [&](const f32x16 (&s)[KB], bf16x8 (&pf)[2 * KB], float& psum)
                          __attribute__((always_inline)) {
       const float m_tile = tile_max(s);
       if (m_tile > m_run) {
@@ -801,7 +831,7 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
       const float mu = m_off();
       psum = 0.f;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < 2 * KB; ++k) {
         float q[8];
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
@@ -813,19 +843,19 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
     };
     // Values that are not finite in a masked tile (see the kernel for few
     // pairs): added where they are seen, then made 0.
-    auto odd_values = [&](const f32x16 (&s)[2], int x, char* sV) __attribute__((always_inline)) {
+    auto odd_values = [&](const f32x16 (&s)[KB], int x, char* sV) __attribute__((always_inline)) {
       bool odd = false;
 #pragma unroll
       for (int j = 0; j < NL; ++j) odd |= odd16(sV + (j * 4 + wave) * 1024 + lane * 16);
       if (!__syncthreads_or(odd)) return;
       const float mu = m_off();
-      const uint32_t see0 = seen(x, 0), see1 = seen(x, 1);
+      const uint32_t see0 = seen(x, 0), see1 = KB > 1 ? seen(x, KB - 1) : 0;
 #pragma nounroll
       for (int key = 0; key < BK; ++key) {
         const int kk = key & 31, rr = (kk >> 3) * 4 + (kk & 3), hh = (kk >> 2) & 1;
         float sk = 0.f;
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < KB; ++b)
 #pragma unroll
           for (int r = 0; r < 16; ++r) sk = b * 16 + r == (key >> 5) * 16 + rr ? s[b][r] : sk;
         sk = __shfl(sk, c + 32 * hh);
@@ -838,27 +868,32 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
       __syncthreads();
     };
 
-    bf16x8 pf[4];
+    bf16x8 pf[2 * KB];
     float psum_a = 0.f;
     if (keys) {
-      locate(0, at_v);
-      issue(kb, at_v, ldsK);
-      issue(vb, at_v, ldsV);
-      locate(min(1, n - 1), at_v);
-      if (n > 1) issue(kb, at_v, ldsK + TB);
-      locate(min(2, n - 1), at_k);
-      wait_loads<0>();
-      __syncthreads();
+      // K 0, V 0, K 1, V 1, .., K NB - 1, and then wait for K 0 alone
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        locate(min(i, n - 1), at_v);
+        if (i < n) issue(kb, at_v, ldsK + i * TB);
+        if (i < n && i + 1 < NB) issue(vb, at_v, ldsV + i * TB);
+      }
+      locate(min(NB, n - 1), at_k);
+      if (NB <= n)
+        wait_loads<(NB - 1) * 2 * NL>();
+      else
+        wait_loads<0>();
+      lds_barrier();
     }
     if (keys && active) {
 #pragma unroll
-      for (int j = 0; j < 2 * KS; ++j)
-        sc[0][j & 1] = mfma32(kfrag(0, j), qf[j >> 1], j < 2 ? f32x16{} : sc[0][j & 1]);
+      for (int j = 0; j < KB * KS; ++j)
+        sc[0][j % KB] = mfma32(kfrag(0, j), qf[j / KB], j < KB ? f32x16{} : sc[0][j % KB]);
       mask_tile(sc[0], 0);
       m_run = tile_max(sc[0]);
       const float mu = m_off();
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
+      for (int k = 0; k < KB; ++k) {
         float q[8];
 #pragma unroll
         for (int u = 0; u < 8; ++u) {
@@ -868,74 +903,77 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
         pf[k] = pack8(q);
       }
     }
-    // One step: tile x (scores in set P, its first two operands in pf) and the
-    // scores of tile x + 1.  On the last tile the score MFMAs run on stale
-    // LDS and their results are dropped.
-    auto step = [&](auto par, int x) __attribute__((always_inline)) {
-      constexpr int P = decltype(par)::value;
-      f32x16 (&cur)[2] = sc[P];
-      f32x16 (&nxt)[2] = sc[P ^ 1];
+    // One step: tile x (in buffer S = x % NB; its scores in set S % 2, the
+    // operands of its first half in pf) and the scores of tile x + 1.  On the
+    // last tile the score MFMAs run on stale LDS and their results are dropped.
+    auto step = [&](auto tag, int x) __attribute__((always_inline)) {
+      constexpr int S = decltype(tag)::value, P = S & 1, S1 = (S + 1) % NB;
+      f32x16 (&cur)[KB] = sc[P];
+      f32x16 (&nxt)[KB] = sc[P ^ 1];
       const bool next = x + 1 < n;   // block-uniform
-      // K of tile x + 1 and V of tile x have landed, every wave is done with
-      // K of tile x and V of tile x - 1
-      wait_loads<0>();
-      __syncthreads();
-      if (x + 2 < n) issue(kb, at_k, ldsK + P * TB);
-      if (next) issue(vb, at_v, ldsV + (P ^ 1) * TB);
+      // K of tile x + 1 and V of tile x have landed (those behind them may be in
+      // flight), every wave is done with K of tile x and V of tile x - 1
+      if (x + NB - 1 < n)
+        wait_loads<(NB - 2) * 2 * NL>();
+      else
+        wait_loads<0>();
+      lds_barrier();
+      if (x + NB < n) issue(kb, at_k, ldsK + S * TB);
+      if (x + NB - 1 < n) issue(vb, at_v, ldsV + (S + NB - 1) % NB * TB);
       const float mu = m_off();
       if (active) {
         float psum = psum_a;
         bf16x8 kr[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) kr[j] = kfrag(P ^ 1, j);
-        float q[16];
+        for (int j = 0; j < 4; ++j) kr[j] = kfrag(S1, j);
+        float q[H];
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int j = 0; j < 2 * KS; ++j) {
-          nxt[j & 1] = mfma32(kr[j & 3], qf[j >> 1], j < 2 ? f32x16{} : nxt[j & 1]);
-          if (j + 4 < 2 * KS) kr[j & 3] = kfrag(P ^ 1, j + 4);
-          constexpr int NS = 2 * KS;
-          const int i0 = 16 * j / NS, i1 = 16 * (j + 1) / NS;
+        for (int j = 0; j < KB * KS; ++j) {
+          nxt[j % KB] = mfma32(kr[j & 3], qf[j / KB], j < KB ? f32x16{} : nxt[j % KB]);
+          if (j + 4 < KB * KS) kr[j & 3] = kfrag(S1, j + 4);
+          constexpr int NS = KB * KS;
+          const int i0 = H * j / NS, i1 = H * (j + 1) / NS;
 #pragma unroll
           for (int i = i0; i < i1; ++i) {
-            q[i] = pexp(cur, 16 + i, mu);
+            q[i] = pexp(cur, H + i, mu);
             psum += q[i];
           }
           if (i1 / 8 != i0 / 8) {
             const int k = i1 / 8 - 1;
-            pf[2 + k] = pack8(q + 8 * k);
-            asm volatile("" : "+v"(pf[2 + k]));
+            pf[KB + k] = pack8(q + 8 * k);
+            asm volatile("" : "+v"(pf[KB + k]));
           }
           __builtin_amdgcn_sched_barrier(0);
         }
         if (__any(!(psum <= 65536.f) || (qok && m_run == -INFINITY))) slow_tile(cur, pf, psum);
         l_run += psum;
       }
-      if (masked(x)) odd_values(cur, x, &sVb[P][0]);
+      if (masked(x)) odd_values(cur, x, &sVb[S][0]);
       if (next && active) mask_tile(nxt, x + 1);
       // the tiles asked for after the next barrier: V follows K
 #pragma unroll
       for (int j = 0; j < NL; ++j) at_v[j] = at_k[j];
-      if (x + 3 < n) {
-        pages.ahead((key_base + (x + 3) * BK) >> a.psl, last);
-        locate(x + 3, at_k);
+      if (x + NB + 1 < n) {
+        pages.ahead((key_base + (x + NB + 1) * BK) >> a.psl, last);
+        locate(x + NB + 1, at_k);
       }
       if (active) {
         const float mu1 = m_off();
-        const char* sV = &sVb[P][0];
+        const char* sV = &sVb[S][0];
         auto vfrag = [&](int st) { return ld_tr_swz<D>(sV, (st / DB) * 16, (st % DB) * 32); };
         bf16x8 vr[4];
 #pragma unroll
         for (int st = 0; st < 4; ++st) vr[st] = vfrag(st);
-        float q[16];
+        float q[H];
         psum_a = 0.f;
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int st = 0; st < 4 * DB; ++st) {
+        for (int st = 0; st < 2 * KB * DB; ++st) {
           oacc[st % DB] = mfma32(vr[st & 3], pf[st / DB], oacc[st % DB]);
-          if (st + 4 < 4 * DB) vr[st & 3] = vfrag(st + 4);
-          constexpr int NS = 4 * DB;
-          const int i0 = 16 * st / NS, i1 = 16 * (st + 1) / NS;
+          if (st + 4 < 2 * KB * DB) vr[st & 3] = vfrag(st + 4);
+          constexpr int NS = 2 * KB * DB;
+          const int i0 = H * st / NS, i1 = H * (st + 1) / NS;
 #pragma unroll
           for (int i = i0; i < i1; ++i) {
             q[i] = pexp(nxt, i, mu1);
@@ -952,11 +990,13 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
       }
     };
     if (keys) {
-      using p0 = std::integral_constant<int, 0>;
-      using p1 = std::integral_constant<int, 1>;
-      for (int x = 0; x < n; x += 2) {
-        step(p0{}, x);
-        if (x + 1 < n) step(p1{}, x + 1);
+      for (int x = 0; x < n; x += NB) {
+        step(std::integral_constant<int, 0>{}, x);
+        if (x + 1 < n) step(std::integral_constant<int, 1>{}, x + 1);
+        if constexpr (NB == 4) {
+          if (x + 2 < n) step(std::integral_constant<int, 2>{}, x + 2);
+          if (x + 3 < n) step(std::integral_constant<int, 3>{}, x + 3);
+        }
       }
     }
     const float l = l_run + __shfl_xor(l_run, 32);
@@ -992,7 +1032,7 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
       }
     }
     deal.note();
-    __syncthreads();   // the tiles are read before the next segment's loads
+    lds_barrier();   // the tiles are read before the next segment's loads
   }
 }
 
@@ -1168,7 +1208,7 @@ static hipError_t launch_tree(const TreePlan& p, TreeArgs a, hipStream_t stream)
   {
     ProfScope prof("tree_attn", stream);
     if (p.many)
-      hipLaunchKernelGGL((tree_many_kernel<D>), dim3(p.groups), dim3(256), 0, stream, a);
+      hipLaunchKernelGGL((tree_many_kernel<D, 2, 2>), dim3(p.groups), dim3(256), 0, stream, a);
     else
       hipLaunchKernelGGL((tree_few_kernel<D, kFewWaves>), dim3(p.groups), dim3(64 * kFewWaves), 0,
                          stream, a);
