@@ -152,13 +152,15 @@ __device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {   // of what
 
 // The deal: every workgroup works out the same one from the lengths, and
 // walks its own run of it, segment by segment.  To begin and end a tile takes
-// about as long as two units (the first keys' way from memory, the result's
-// way back), so where runs are long a tile counts for that many more: without
-// it, 4000 rows of a prompt over no context took 234 us, runs of many short
-// tiles being the last to end, and 64 rollouts' decode 111.
+// as long as several units (the first keys' way from memory, masked units, the
+// result's way back), so where runs are long a tile counts for that many more:
+// without it runs of many short tiles were the last to end (us, counting a tile
+// for 0 / 2 / 4 / 6 more: 4000 rows of a prompt over no context, 28/4 heads,
+// 234 / 187 / 168 / 155; 64 rollouts' decode over 257 to 16384 keys
+// 111 / 103 / 101 / 102; 128 over 250 to 1000 keys - / 37.3 / 37.9 / 41.1).
 // AGAIN: the arguments are read from where they were passed each time (the
 // kernel has no scalar registers to hold them in).
-constexpr int kTileCost = 2, kLongRun = 8;
+constexpr int kTileCostMany = 6, kTileCostFew = 4, kLongRun = 8;
 
 template <int R, int BLOCK, bool AGAIN>
 struct Deal {
@@ -222,7 +224,8 @@ struct Deal {
     }
     units = uniform(units);
     tiles = uniform(tiles);
-    extra = units * a.Hkv >= int64_t(kLongRun) * a.groups ? kTileCost : 0;
+    extra = units * a.Hkv >= int64_t(kLongRun) * a.groups
+                ? (R == 128 ? kTileCostMany : kTileCostFew) : 0;
     total = units + extra * tiles;
     per = max(int64_t(1), quotient(total * a.Hkv + a.groups - 1, a.groups));
     begin = run * per;
