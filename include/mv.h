@@ -752,7 +752,8 @@ mv_status mv_cache_free(const mv_cache_shape* shape, const mv_cache* cache, int3
  * seq_ids[b], already written; with c = seq_len - n, its row i is at cache
  * row c + i.  Row i sees every row before c and, of the new ones, itself and
  * those before it (tree == null), or those whose bit is set in its words of
- * `tree`: bit a % 32 of word a / 32 stands for new row a of the same entry.
+ * `tree`: bit a % 32 of word a / 32 stands for new row a of the same entry (a
+ * row past its words is not seen).
  *     o = softmax(scale * q.k) v,   lse = log sum exp(scale * q.k)
  * over the rows seen; a row that sees none (seq_ids -1 or out of range, a
  * sequence shorter than n) gets o = 0, lse = -inf.  What a row does not see
@@ -760,7 +761,10 @@ mv_status mv_cache_free(const mv_cache_shape* shape, const mv_cache* cache, int3
  * q, o bf16 [n_rows, n_heads_q, head_dim]; lse fp32 [n_heads_q, n_rows];
  * row_ptr int32 [n_batch + 1], row_ptr[0] = 0, non-decreasing, at most n_rows;
  * rows from row_ptr[n_batch] on are left as they were.
- * A sequence may occur in several entries.  Deterministic.
+ * A sequence may occur in several entries.  An entry that mv_cache_reserve
+ * refused has no new rows to attend from.  Deterministic: the same call gives
+ * the same bits.  At most MV_CACHE_MAX_SEQS entries, and some 7 million (row,
+ * query head) pairs per KV head.
  * ------------------------------------------------------------------------ */
 typedef struct {
   int32_t n_batch, n_rows, n_heads_q;

@@ -216,7 +216,7 @@ const char* mv_status_string(mv_status s) {
 
 const char* mv_last_error(void) { return mv::g_last_error.c_str(); }
 
-int32_t mv_version(void) { return (1 << 16) | 0; }
+int32_t mv_version(void) { return (1 << 16) | 1; }
 
 mv_status mv_view_mask_materialize(const mv_view_mask* m, int32_t row_begin, int32_t row_end,
                                    uint32_t* dev_bits, hipStream_t stream) {

@@ -881,16 +881,21 @@ class PagedCache:
         if not mv_cache_compact_workspace_bytes(ctypes.byref(self.shape), 0):
             check(mv_cache_reset(ctypes.byref(self.shape), None, None))
         pool = (n_layers, n_pages, n_heads_kv, page_size, head_dim)
-        self.k = torch.empty(pool, dtype=torch.bfloat16, device=device)
-        self.v = torch.empty(pool, dtype=torch.bfloat16, device=device)
         i32 = lambda *s: torch.empty(s, dtype=torch.int32, device=device)
-        self.page_table, self.seq_len = i32(n_seqs, max_pages), i32(n_seqs)
-        self.page_refs, self._ctl = i32(n_pages), i32(4)
-        self.c = CacheC(_ptr(self.k), _ptr(self.v), _ptr(self.page_table), _ptr(self.seq_len),
-                        _ptr(self.page_refs), _ptr(self._ctl))
-        self._dev, self.head_dim = self.k.get_device(), int(head_dim)
+        pools = [torch.empty(pool, dtype=torch.bfloat16, device=device) for _ in range(2)]
+        self._t = (*pools, i32(n_seqs, max_pages), i32(n_seqs), i32(n_pages), i32(4))
+        self.c = CacheC(*[_ptr(t) for t in self._t])
+        self._dev, self.head_dim = pools[0].get_device(), int(head_dim)
         self._refs = (ctypes.byref(self.shape), ctypes.byref(self.c))
         self.reset(stream)
+
+    # (the library holds their addresses: their contents may be set, they
+    # themselves not)
+    k = property(lambda self: self._t[0])
+    v = property(lambda self: self._t[1])
+    page_table = property(lambda self: self._t[2])
+    seq_len = property(lambda self: self._t[3])
+    page_refs = property(lambda self: self._t[4])
 
     def _args(self):
         if self._dev != _device():
@@ -900,9 +905,7 @@ class PagedCache:
 
     def reset(self, stream=None) -> None:
         """Every sequence empty, every page free."""
-        check(mv_cache_reset(*self._args(),
-                             _use(stream, self.k, self.v, self.page_table, self.seq_len,
-                                  self.page_refs, self._ctl)))
+        check(mv_cache_reset(*self._args(), _use(stream, *self._t)))
 
     def restore(self, page_table, seq_len, page_refs) -> None:
         """Take over a state saved from (or laid out for) a cache of this shape."""
@@ -912,7 +915,7 @@ class PagedCache:
             if tuple(mine.shape) != tuple(theirs.shape):
                 raise ValueError(f"{what}: expected shape {tuple(mine.shape)}")
             mine.copy_(theirs)
-        self._ctl.zero_()
+        self._t[5].zero_()
 
     def status(self, stream=None) -> dict:
         """free_pages, and the entries refused (for lack of pages, as malformed)
@@ -920,6 +923,13 @@ class PagedCache:
         out = CacheCounts()
         check(mv_cache_status(*self._args(), ctypes.byref(out), _stream(stream)))
         return out.as_dict()
+
+
+def _workspace(given, make):
+    if given is None:
+        return make()
+    _need(given, torch.uint8, "workspace")
+    return given
 
 
 def _need_ids(t, what, n=None):
@@ -973,7 +983,7 @@ def cache_fork(cache: PagedCache, src, dst, share: bool = True, workspace=None,
     (or copied too)."""
     n = _need_ids(src, "src")
     _need_ids(dst, "dst", n)
-    ws = workspace if workspace is not None else cache_workspace(cache, n)
+    ws = _workspace(workspace, lambda: cache_workspace(cache, n))
     check(mv_cache_fork(*cache._args(), n, src.data_ptr(), dst.data_ptr(), 1 if share else 0,
                         ws.data_ptr(), ws.numel(),
                         _use(stream, ws if workspace is None else None)))
@@ -989,7 +999,7 @@ def cache_compact(cache: PagedCache, src, dst, span_ptr, spans, workspace=None,
     _need(spans, torch.int32, "spans")
     if spans.dim() != 2 or spans.shape[1] != 2:
         raise ValueError("spans: expected [n_spans, 2]")
-    ws = workspace if workspace is not None else cache_workspace(cache, n)
+    ws = _workspace(workspace, lambda: cache_workspace(cache, n))
     check(mv_cache_compact(*cache._args(), n, _ptr(src), _ptr(dst), _ptr(span_ptr), _ptr(spans),
                            spans.shape[0], _ptr(ws), ws.numel(),
                            _use(stream, ws if workspace is None else None)))
@@ -1061,10 +1071,8 @@ def tree_attn(cache: PagedCache, layer: int, q, seq_ids, row_ptr, tree=None,
         o, lse = out
         _need(o, torch.bfloat16, "o", dims)
         _need(lse, torch.float32, "lse", (heads, n))
-    ws = workspace
-    if ws is None:
-        ws = torch.empty(int(mv_tree_attn_workspace_bytes(refs[0], shape)), dtype=torch.uint8,
-                         device=dev)
+    ws = _workspace(workspace, lambda: torch.empty(
+        int(mv_tree_attn_workspace_bytes(refs[0], shape)), dtype=torch.uint8, device=dev))
     handle = _stream(stream) if stream is None else _use(
         stream, *((o, lse) if out is None else ()), *((ws,) if workspace is None else ()))
     check(mv_tree_attn(*refs, int(layer), shape, seq_ids.data_ptr(), row_ptr.data_ptr(),
