@@ -406,6 +406,13 @@ template <int N>
 __device__ __forceinline__ void wait_loads() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
+// Operands loaded before a loop are waited for here: left to itself the compiler
+// waits at their first use inside it, for every load in flight, each time round.
+template <int N>
+__device__ __forceinline__ void settle(bf16x8 (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(v[i]));
+}
 __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 __device__ __forceinline__ bool odd_bf16x2(uint32_t w) {   // one of two is not finite
@@ -528,6 +535,7 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
       pages.start(key_of(0), last);
       wait_loads<0>();
     }
+    settle(qf);
     // Tile x of this wave into buffer x & 1.  Rows past the last key are read
     // from the last key's page (what they hold is masked).
     auto issue = [&](int x) {
@@ -761,6 +769,7 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
       pages.start(key_base, last);
       wait_loads<0>();
     }
+    settle(qf);
     // The rows (of the layer's pool, from the KV head's first) that this wave
     // loads of tile x.  Rows past the last key are read from the last key's page
     // (what they hold is masked).

@@ -1065,7 +1065,7 @@ def tree_attn(cache: PagedCache, layer: int, q, seq_ids, row_ptr, tree=None,
                                        float(scale) if scale else 0.0))
     refs, dev = cache._args(), q.device
     if out is None:
-        o = torch.empty(dims, dtype=torch.bfloat16, device=dev)
+        o = torch.empty_like(q)
         lse = torch.empty((heads, n), dtype=torch.float32, device=dev)
     else:
         o, lse = out
