@@ -44,7 +44,15 @@ struct TreeArgs {
   int tiles;           // tile places: at least as many as there are tiles
   int groups;          // workgroups
   float scale_log2;
+  uint32_t g_mul;      // for by_heads
+  int g_shift;
 };
+
+// x / G for 0 <= x < 2^31 by a product: g_mul = ceil(2^g_shift / G) with
+// 2^(g_shift - 31) >= G, so that what it is too large by adds less than 1 / G.
+__device__ __forceinline__ int by_heads(const TreeArgs& a, int x) {
+  return int(uint64_t(uint32_t(x)) * a.g_mul >> a.g_shift);
+}
 
 // What is to be joined of a tile place and KV head: the tile's first segment,
 // of run `run`, is at `slot`, that of run r > run at 2 r.
@@ -74,7 +82,7 @@ struct Tile {
 struct TreeShared {
   int ptr[kPlanB + 1];
   int id[kPlanB], len[kPlanB];
-  int tmp[17];
+  int tmp[2][4];
   int64_t units[kChunks], tiles[kChunks];   // before each BLOCK of places
   Tile tile;                    // where a run begins
   int at;
@@ -114,7 +122,7 @@ __device__ __forceinline__ Tile tile_at(const TreeArgs& a, const TreeShared& s, 
   if (t.rows == 0) return t;
   const int L = a.B <= kPlanB ? s.len[b] : entry_len(a, a.ids[b]);
   t.c = L - t.n;
-  const int last = (m0 + t.rows - 1) / a.G;
+  const int last = by_heads(a, m0 + t.rows - 1);
   t.kmax = a.tree ? L : max(0, t.c + last + 1);
   return t;
 }
@@ -192,8 +200,27 @@ struct Deal {
       for (int h = 0; h < a.Hkv; ++h) a.join[int64_t(u) * a.Hkv + h].rows = 0;
     // (a tile has fewer than 2^25 units: BLOCK of them do not pass 2^31 unless
     // the caches are past any memory, in which case the rows are unspecified)
-    before[0] = block_scan<BLOCK>(mine.units(), s.tmp, sum[0]);
-    before[1] = block_scan<BLOCK>(mine.rows > 0, s.tmp, sum[1]);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int units = mine.units(), x = wave_scan(units);
+    const uint64_t is = __ballot(mine.rows > 0);
+    lds_barrier();   // tmp of an earlier block of places is read
+    if (lane == 63) {
+      s.tmp[0][wave] = x;
+      s.tmp[1][wave] = __popcll(is);
+    }
+    lds_barrier();
+    before[0] = x - units;
+    before[1] = __popcll(is & ((uint64_t(1) << lane) - 1));
+    sum[0] = sum[1] = 0;
+#pragma unroll
+    for (int w = 0; w < BLOCK / 64; ++w) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int n = s.tmp[e][w];
+        before[e] += w < wave ? n : 0;
+        sum[e] += n;
+      }
+    }
   }
 
   __device__ __forceinline__ Deal(const TreeArgs& a0, TreeShared& sh, int r)
@@ -462,7 +489,7 @@ struct Pair {
   int i, h;
   int64_t row;
   __device__ __forceinline__ Pair(const TreeArgs& a, const Tile& t, int hk, int m) {
-    i = m / a.G;
+    i = by_heads(a, m);
     h = hk * a.G + m - i * a.G;
     row = int64_t(t.r0) + i;
   }
@@ -558,7 +585,7 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
     };
     if (todo > 0) issue(0);
     if (todo > 1) issue(1);
-    const int clear = a.tree ? t.c : t.c + t.m0 / a.G + 1;   // keys every row of the tile sees
+    const int clear = a.tree ? t.c : t.c + by_heads(a, t.m0) + 1;   // keys every row of the tile sees
     for (int x = 0; x < todo; ++x) {
       // the tile has landed (the next one's loads may be in flight)
       if (x + 1 < todo)
@@ -789,7 +816,7 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
     auto kfrag = [&](int buf, int j) {
       return ld_row_swz<D>(&sKb[buf][0], (j % KB) * 32 + c, (j / KB) * 2 + g);
     };
-    const int clear = a.tree ? t.c : t.c + t.m0 / a.G + 1;   // keys every row of the tile sees
+    const int clear = a.tree ? t.c : t.c + by_heads(a, t.m0) + 1;   // keys every row of the tile sees
     auto masked = [&](int x) { return key_base + x * BK + BK > min(clear, t.kmax); };
     auto seen = [&](int x, int kb2) {   // of keys 32 kb2 .. + 32 of tile x
       const int key0 = key_base + x * BK + kb2 * 32, m = t.kmax - key0;
@@ -1277,6 +1304,9 @@ hipError_t launch_tree_attn(const mv_cache_shape& cs, const CacheDev& cd, int la
   a.Hq = s.n_heads_q;
   a.Hkv = cs.n_heads_kv;
   a.G = s.n_heads_q / cs.n_heads_kv;
+  a.g_shift = 31;
+  while ((1 << (a.g_shift - 31)) < a.G) ++a.g_shift;
+  a.g_mul = uint32_t(((uint64_t(1) << a.g_shift) + a.G - 1) / a.G);
   a.n_pages = cs.n_pages;
   a.n_seqs = cs.n_seqs;
   a.max_pages = cs.max_pages;
