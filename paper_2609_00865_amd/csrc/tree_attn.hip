@@ -105,8 +105,24 @@ __device__ __forceinline__ int entry_len(const TreeArgs& a, int id) {
              ? int(min(int64_t(max(a.len[id], 0)), int64_t(a.max_pages) << a.psl)) : 0;
 }
 
+// A value that is worked out here, not before a loop and held in registers.
+__device__ __forceinline__ int here(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// A value read from LDS here and now: a choice between it and one from memory
+// would otherwise become one load by a generic address, which waits for both.
+__device__ __forceinline__ int from_lds(const int& x) { return here(x); }
+
 __device__ __forceinline__ int first_row(const TreeArgs& a, const TreeShared& s, int b) {
-  return a.B <= kPlanB ? s.ptr[b] : min(max(a.ptr[b], 0), a.N);
+  if (a.B <= kPlanB) return from_lds(s.ptr[b]);
+  return min(max(a.ptr[b], 0), a.N);
+}
+
+__device__ __forceinline__ int entry_id(const TreeArgs& a, const TreeShared& s, int b) {
+  if (a.B <= kPlanB) return from_lds(s.id[b]);
+  return a.ids[b];
 }
 
 // The tile of entry b whose first pair is m0.
@@ -120,7 +136,7 @@ __device__ __forceinline__ Tile tile_at(const TreeArgs& a, const TreeShared& s, 
   t.rows = m0 >= 0 ? max(0, min(R, t.n * a.G - m0)) : 0;
   t.kmax = t.c = 0;
   if (t.rows == 0) return t;
-  const int L = a.B <= kPlanB ? s.len[b] : entry_len(a, a.ids[b]);
+  const int L = a.B <= kPlanB ? from_lds(s.len[b]) : entry_len(a, a.ids[b]);
   t.c = L - t.n;
   const int last = by_heads(a, m0 + t.rows - 1);
   t.kmax = a.tree ? L : max(0, t.c + last + 1);
@@ -325,8 +341,7 @@ struct Deal {
 
   __device__ __forceinline__ const int32_t* pages() const {   // the sequence's row of the table
     const TreeArgs& a = args();
-    const int id = uniform(a.B <= kPlanB ? s.id[t.b] : a.ids[t.b]);
-    return a.table + int64_t(id) * a.max_pages;
+    return a.table + int64_t(uniform(entry_id(a, s, t.b))) * a.max_pages;
   }
 
   // For the join: by the segment that a tile begins with
@@ -362,10 +377,14 @@ __device__ __forceinline__ float weight(float m, float M) {
   return m == -INFINITY ? 1.f : fast_exp2(m - M);
 }
 
-// lse from a maximum (base 2) and the sum beside it, in 64 bits: once a row, and
-// the fp32 logarithm alone would be off by as much as all before it.
+// lse from a maximum (base 2) and the sum beside it.  The sum's exponent and the
+// maximum are added in 64 bits: in 32 their sum would be off by as much as all
+// before it.  What is left of the sum has a logarithm in [-1, 0].
 __device__ __forceinline__ float lse_of(float M, float l) {
-  return l == 0.f ? -INFINITY : float(double(M) * 0.6931471805599453 + log(double(l)));
+  if (l == 0.f) return -INFINITY;
+  const double log2_l = double(__builtin_amdgcn_frexp_expf(l)) +
+                        double(__builtin_amdgcn_logf(__builtin_amdgcn_frexp_mantf(l)));
+  return float((double(M) + log2_l) * 0.6931471805599453);
 }
 
 // The keys of [key0, key0 + 32) that new row i of a tile's entry sees, as
@@ -532,13 +551,9 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
     const int hk = deal.hk;
 
     // Q^T as the B operand: lane holds pair c, dims ks*16 + g*8 .. + 8
-    const bool qok = c < t.rows;
-    const Pair mine(a, t, hk, t.m0 + (qok ? c : 0));
+    // (loaded below; lanes past the tile's pairs hold its first, and store nothing)
+    const Pair mine(a, t, hk, t.m0 + (c < t.rows ? c : 0));
     bf16x8 qf[KS];
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-      qf[ks] = as_bf16x8(qok ? ld16(a.q + (mine.row * a.Hq + mine.h) * D + ks * 16 + g * 8)
-                             : make_uint4(0, 0, 0, 0));
     f32x16 oacc[DB];
 #pragma unroll
     for (int db = 0; db < DB; ++db)
@@ -560,9 +575,11 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
     if (todo > 0) {
       pages.row = deal.pages();
       pages.start(key_of(0), last);
-      wait_loads<0>();
     }
-    settle(qf);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+      qf[ks] = as_bf16x8(ld16(a.q + (mine.row * a.Hq + mine.h) * D + ks * 16 + g * 8));
+    wait_loads<KS>();   // the page ids have landed, Q may be on its way
     // Tile x of this wave into buffer x & 1.  Rows past the last key are read
     // from the last key's page (what they hold is masked).
     auto issue = [&](int x) {
@@ -584,6 +601,8 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
       }
     };
     if (todo > 0) issue(0);
+    wait_loads<0>();
+    settle(qf);
     if (todo > 1) issue(1);
     const int clear = a.tree ? t.c : t.c + by_heads(a, t.m0) + 1;   // keys every row of the tile sees
     for (int x = 0; x < todo; ++x) {
@@ -761,19 +780,8 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
     const bool active = wv * 32 < t.rows;
     // this lane's pair, worked out again where it is needed rather than held
     auto pair = [&](const TreeArgs& b) {
-      int m = t.m0 + (my < t.rows ? my : 0);
-      asm volatile("" : "+v"(m));
-      return Pair(b, t, hk, m);
+      return Pair(b, t, hk, here(t.m0 + (my < t.rows ? my : 0)));
     };
-    bf16x8 qf[KS];
-    {
-      const TreeArgs& b = again();
-      const Pair mine = pair(b);
-      const u16* qp = b.q + (mine.row * b.Hq + mine.h) * D + g * 8;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
-        qf[ks] = as_bf16x8(qok ? ld16(qp + ks * 16) : make_uint4(0, 0, 0, 0));
-    }
     f32x16 oacc[DB];
 #pragma unroll
     for (int db = 0; db < DB; ++db)
@@ -794,9 +802,17 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
     if (keys) {
       pages.row = deal.pages();
       pages.start(key_base, last);
-      wait_loads<0>();
     }
-    settle(qf);
+    // (lanes past the tile's pairs hold its first, and store nothing)
+    bf16x8 qf[KS];
+    {
+      const TreeArgs& b = again();
+      const Pair mine = pair(b);
+      const u16* qp = b.q + (mine.row * b.Hq + mine.h) * D + here(g) * 8;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) qf[ks] = as_bf16x8(ld16(qp + ks * 16));
+    }
+    wait_loads<KS>();   // the page ids have landed, Q may be on its way
     // The rows (of the layer's pool, from the KV head's first) that this wave
     // loads of tile x.  Rows past the last key are read from the last key's page
     // (what they hold is masked).
@@ -910,18 +926,16 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
     bf16x8 pf[2 * KB];
     float psum_a = 0.f;
     if (keys) {
-      // K 0, V 0, K 1, V 1, .., K NB - 1, and then wait for K 0 alone
-#pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        locate(min(i, n - 1), at_v);
-        if (i < n) issue(kb, at_v, ldsK + i * TB);
-        if (i < n && i + 1 < NB) issue(vb, at_v, ldsV + i * TB);
-      }
-      locate(min(NB, n - 1), at_k);
-      if (NB <= n)
-        wait_loads<(NB - 1) * 2 * NL>();
-      else
-        wait_loads<0>();
+      locate(0, at_v);
+      issue(kb, at_v, ldsK);
+      issue(vb, at_v, ldsV);
+    }
+    wait_loads<0>();
+    settle(qf);
+    if (keys) {
+      locate(min(1, n - 1), at_v);
+      if (n > 1) issue(kb, at_v, ldsK + TB);
+      locate(min(2, n - 1), at_k);
       lds_barrier();
     }
     if (keys && active) {
@@ -1044,24 +1058,24 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
       const Pair mine = pair(b);
       if (deal.whole()) {
         const float inv = l == 0.f ? 0.f : 1.f / l;   // l is 0 where no key was seen
-        u16* op = b.o + (mine.row * b.Hq + mine.h) * D;
+        u16* op = b.o + (mine.row * b.Hq + mine.h) * D + here(g) * 4;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
           for (int q4 = 0; q4 < 4; ++q4)
-            *reinterpret_cast<uint2*>(op + db * 32 + q4 * 8 + g * 4) =
+            *reinterpret_cast<uint2*>(op + db * 32 + q4 * 8) =
                 make_uint2(pack2(oacc[db][q4 * 4 + 0] * inv, oacc[db][q4 * 4 + 1] * inv),
                            pack2(oacc[db][q4 * 4 + 2] * inv, oacc[db][q4 * 4 + 3] * inv));
         if (g == 0)
           b.lse[int64_t(mine.h) * b.N + mine.row] = lse_of(m_run, l);
       } else {
-        const int64_t s = deal.slot() * R + my;
-        float* op = b.part_o + s * D;
+        const int64_t s = deal.slot() * R + here(my);
+        float* op = b.part_o + s * D + here(g) * 4;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
           for (int q4 = 0; q4 < 4; ++q4)
-            *reinterpret_cast<float4*>(op + db * 32 + q4 * 8 + g * 4) =
+            *reinterpret_cast<float4*>(op + db * 32 + q4 * 8) =
                 make_float4(oacc[db][q4 * 4 + 0], oacc[db][q4 * 4 + 1], oacc[db][q4 * 4 + 2],
                             oacc[db][q4 * 4 + 3]);
         if (g == 0) {
