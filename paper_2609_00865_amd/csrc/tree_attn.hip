@@ -105,6 +105,10 @@ __device__ __forceinline__ int entry_len(const TreeArgs& a, int id) {
              ? int(min(int64_t(max(a.len[id], 0)), int64_t(a.max_pages) << a.psl)) : 0;
 }
 
+__device__ __forceinline__ uint32_t read_lane(uint32_t x, int lane) {
+  return uint32_t(__builtin_amdgcn_readlane(int(x), lane));
+}
+
 // A value that is worked out here, not before a loop and held in registers.
 __device__ __forceinline__ int here(int x) {
   asm volatile("" : "+v"(x));
@@ -442,11 +446,26 @@ struct PageRing {
   __device__ __forceinline__ void ahead(int j, int last) {
     if ((j >> 6) == window) load(window + 1, last >> psl);
   }
-  __device__ __forceinline__ int64_t get(int j) const {
-    const unsigned p = __builtin_amdgcn_readfirstlane(slots[((j >> 6) & 1) * 64 + (j & 63)]);
-    return p < unsigned(n_pages) ? p : 0;
+  // The row of the layer's pool (from the KV head's first) that holds a key, a
+  // page having page_rows; a key past the last is read from the last one's page.
+  // (Each lane its own: the look-ups of a tile are one, their results read by lane.)
+  __device__ __forceinline__ uint32_t row_of(int key, int last, uint32_t page_rows) const {
+    const int j = min(key, last) >> psl;
+    const unsigned p = slots[j & 127];
+    return (p < unsigned(n_pages) ? p : 0) * page_rows + (key & ((1 << psl) - 1));
   }
 };
+
+// lds_load16s with an LDS address that is in a scalar register as it is
+__device__ __forceinline__ void lds_load16u(const void* base, uint32_t off, uint32_t lds) {
+  uint32_t saved;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\tglobal_load_lds_dwordx4 %1, %2\n\t"
+      "s_mov_b32 m0, %0"
+      : "=&s"(saved)
+      : "v"(off), "s"(base), "s"(lds)
+      : "memory");
+}
 
 template <int N>
 __device__ __forceinline__ void wait_loads() {
@@ -568,7 +587,7 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
     const int todo = nt > wv ? (nt - wv + NW - 1) / NW : 0;
     auto key_of = [&](int x) { return k_begin + (wv + x * NW) * 32; };
     const int last = t.kmax - 1;
-    const int64_t page_bytes = int64_t(a.Hkv) * ps * D * 2;
+    const uint32_t page_rows = uint32_t(a.Hkv) * ps;   // (a pool of 2^32 rows is past any memory)
     const char* kb = reinterpret_cast<const char*>(a.k) + int64_t(hk) * ps * D * 2;
     const char* vb = reinterpret_cast<const char*>(a.v) + int64_t(hk) * ps * D * 2;
     PageRing pages{nullptr, lds_addr(&pg[wave][0]), &pg[wave][0], 0, a.n_pages, a.psl};
@@ -586,16 +605,11 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
       const int key0 = key_of(x);
       pages.ahead(key0 >> a.psl, last);
       const uint32_t kl = lds0 + uint32_t(x & 1) * TB;
-      // (16 rows of a page at a time: the look-ups of a tile wait together)
-      int64_t at[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int key = key0 + j * 16;
-        at[j] = pages.get(min(key, last) >> a.psl) * page_bytes + (key & (ps - 1)) * (D * 2);
-      }
+      // (16 rows of a page at a time)
+      const uint32_t at = pages.row_of(key0 + (lane & 1) * 16, last, page_rows);
 #pragma unroll
       for (int j = 0; j < NI; ++j) {
-        const int64_t x0 = at[j / NO] + (j % NO) * 1024;
+        const int64_t x0 = int64_t(read_lane(at, j / NO)) * (D * 2) + (j % NO) * 1024;
         lds_load16s(kb + x0, voff[j % NO], kl + j * 1024);
         lds_load16s(vb + x0, voff[j % NO], kl + 2 * TB + j * 1024);
       }
@@ -768,19 +782,23 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
   // one offset per lane serves all, the rest of the address is scalar.
   const int wv = uniform(wave), lrow = lane / (D / 8);
   const uint32_t voff = uint32_t(lrow * D * 2 + ((lane % (D / 8) ^ kv_swz<D>(wv * LR + lrow)) << 4));
-  const uint32_t ldsK = lds_addr(&sKb[0][0]) + wv * 1024, ldsV = lds_addr(&sVb[0][0]) + wv * 1024;
+  const uint32_t ldsK = uniform(int(lds_addr(&sKb[0][0]) + wv * 1024));
+  const uint32_t ldsV = uniform(int(lds_addr(&sVb[0][0]) + wv * 1024));
 
   for (; !deal.done(); deal.next()) {
     const Tile& t = deal.t;
     const int hk = deal.hk;
 
-    const int my = wave * 32 + c;
-    const bool qok = my < t.rows;
+    auto my = [&]() {   // this lane's pair of the tile
+      const int x = here(threadIdx.x);
+      return (x >> 6) * 32 + (x & 31);
+    };
     // a wave without pairs loads its share of the tiles and computes nothing
     const bool active = wv * 32 < t.rows;
     // this lane's pair, worked out again where it is needed rather than held
     auto pair = [&](const TreeArgs& b) {
-      return Pair(b, t, hk, here(t.m0 + (my < t.rows ? my : 0)));
+      const int m = my();
+      return Pair(b, t, hk, t.m0 + (m < t.rows ? m : 0));
     };
     f32x16 oacc[DB];
 #pragma unroll
@@ -797,7 +815,7 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
     const uint32_t page_rows = uint32_t(a.Hkv) * ps;   // (a pool of 2^32 rows is past any memory)
     const char* kb = reinterpret_cast<const char*>(a.k) + int64_t(hk) * ps * D * 2;
     const char* vb = reinterpret_cast<const char*>(a.v) + int64_t(hk) * ps * D * 2;
-    PageRing pages{nullptr, lds_addr(&pg[wave][0]), &pg[wave][0], 0, a.n_pages, a.psl};
+    PageRing pages{nullptr, lds_addr(&pg[wv][0]), &pg[wv][0], 0, a.n_pages, a.psl};
     const bool keys = t.kmax > 0;   // block-uniform
     if (keys) {
       pages.row = deal.pages();
@@ -813,22 +831,17 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
       for (int ks = 0; ks < KS; ++ks) qf[ks] = as_bf16x8(ld16(qp + ks * 16));
     }
     wait_loads<KS>();   // the page ids have landed, Q may be on its way
-    // The rows (of the layer's pool, from the KV head's first) that this wave
-    // loads of tile x.  Rows past the last key are read from the last key's page
-    // (what they hold is masked).
-    auto locate = [&](int x, uint32_t (&at)[NL]) {
-#pragma unroll
-      for (int j = 0; j < NL; ++j) {
-        const int key = key_base + x * BK + (j * 4 + wv) * LR;
-        at[j] = uint32_t(pages.get(min(key, last) >> a.psl)) * page_rows + (key & (ps - 1));
-      }
+    // The first rows of this wave's loads of tile x.  (What rows past the last
+    // key hold is masked.)
+    auto locate = [&](int x) {   // lane j: load j
+      return pages.row_of(key_base + x * BK + ((lane & (NL - 1)) * 4 + wv) * LR, last, page_rows);
     };
-    auto issue = [&](const char* base, const uint32_t (&at)[NL], uint32_t lds) {
+    auto issue = [&](const char* base, uint32_t at, uint32_t lds) {
 #pragma unroll
       for (int j = 0; j < NL; ++j)
-        lds_load16s(base + uint64_t(at[j]) * (D * 2), voff, lds + j * 4096);
+        lds_load16u(base + uint64_t(read_lane(at, j)) * (D * 2), voff, lds + j * 4096);
     };
-    uint32_t at_v[NL], at_k[NL];   // of the V tile and of the K tile to be asked for next
+    uint32_t at_v, at_k;   // of the V tile and of the K tile to be asked for next
     auto kfrag = [&](int buf, int j) {
       return ld_row_swz<D>(&sKb[buf][0], (j % KB) * 32 + c, (j / KB) * 2 + g);
     };
@@ -901,7 +914,7 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
     auto odd_values = [&](const f32x16 (&s)[KB], int x, char* sV) __attribute__((always_inline)) {
       bool odd = false;
 #pragma unroll
-      for (int j = 0; j < NL; ++j) odd |= odd16(sV + (j * 4 + wave) * 1024 + lane * 16);
+      for (int j = 0; j < NL; ++j) odd |= odd16(sV + (j * 4 + wv) * 1024 + (here(threadIdx.x) & 63) * 16);
       if (!__syncthreads_or(odd)) return;
       const float mu = m_off();
       const uint32_t see0 = seen(x, 0), see1 = KB > 1 ? seen(x, KB - 1) : 0;
@@ -919,23 +932,23 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
       }
       __syncthreads();
 #pragma unroll
-      for (int j = 0; j < NL; ++j) clear_odd16(sV + (j * 4 + wave) * 1024 + lane * 16);
+      for (int j = 0; j < NL; ++j) clear_odd16(sV + (j * 4 + wv) * 1024 + (here(threadIdx.x) & 63) * 16);
       __syncthreads();
     };
 
     bf16x8 pf[2 * KB];
     float psum_a = 0.f;
     if (keys) {
-      locate(0, at_v);
+      at_v = locate(0);
       issue(kb, at_v, ldsK);
       issue(vb, at_v, ldsV);
     }
     wait_loads<0>();
     settle(qf);
     if (keys) {
-      locate(min(1, n - 1), at_v);
+      at_v = locate(min(1, n - 1));
       if (n > 1) issue(kb, at_v, ldsK + TB);
-      locate(min(2, n - 1), at_k);
+      at_k = locate(min(2, n - 1));
       lds_barrier();
     }
     if (keys && active) {
@@ -999,17 +1012,16 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
           }
           __builtin_amdgcn_sched_barrier(0);
         }
-        if (__any(!(psum <= 65536.f) || (qok && m_run == -INFINITY))) slow_tile(cur, pf, psum);
+        if (__any(!(psum <= 65536.f) || m_run == -INFINITY)) slow_tile(cur, pf, psum);
         l_run += psum;
       }
       if (masked(x)) odd_values(cur, x, &sVb[S][0]);
       if (next && active) mask_tile(nxt, x + 1);
       // the tiles asked for after the next barrier: V follows K
-#pragma unroll
-      for (int j = 0; j < NL; ++j) at_v[j] = at_k[j];
+      at_v = at_k;
       if (x + NB + 1 < n) {
         pages.ahead((key_base + (x + NB + 1) * BK) >> a.psl, last);
-        locate(x + NB + 1, at_k);
+        at_k = locate(x + NB + 1);
       }
       if (active) {
         const float mu1 = m_off();
@@ -1053,7 +1065,7 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
       }
     }
     const float l = l_run + __shfl_xor(l_run, 32);
-    if (qok) {
+    if (const int m = my(); m < t.rows) {
       const TreeArgs& b = again();
       const Pair mine = pair(b);
       if (deal.whole()) {
@@ -1069,7 +1081,7 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
         if (g == 0)
           b.lse[int64_t(mine.h) * b.N + mine.row] = lse_of(m_run, l);
       } else {
-        const int64_t s = deal.slot() * R + here(my);
+        const int64_t s = deal.slot() * R + m;
         float* op = b.part_o + s * D + here(g) * 4;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
