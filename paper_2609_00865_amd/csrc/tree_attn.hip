@@ -757,20 +757,19 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
 }
 
 // --------------------------------------------------------------------------
-// many pairs: four waves of 32 pairs on shared tiles of 32 KB keys, K and V in
-// NB buffers each
+// many pairs: four waves of 32 pairs on shared tiles of 64 keys, K and V in two
+// buffers each
 // --------------------------------------------------------------------------
-template <int D, int KB, int NB>
+template <int D>
 __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
-  constexpr int R = 128, BK = 32 * KB, BLOCK = 256;
+  constexpr int R = 128, KB = 2, BK = 32 * KB, BLOCK = 256;
   constexpr int KS = D / 16, DB = D / 32;
   constexpr int TB = BK * D * 2;             // bytes of a tile
   constexpr int NL = TB / 4096;              // loads of a thread per tile
   constexpr int LR = 512 / D;                // rows of a wave's load
   constexpr int H = 8 * KB;                  // half the elements of a tile in a lane
-  static_assert(NB % 2 == 0, "score sets take turns with the buffers");
-  __shared__ __align__(1024) char sKb[NB][TB];
-  __shared__ __align__(1024) char sVb[NB][TB];
+  __shared__ __align__(1024) char sKb[2][TB];
+  __shared__ __align__(1024) char sVb[2][TB];
   __shared__ __align__(16) int pg[4][128];
   __shared__ TreeShared sh;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
@@ -917,7 +916,7 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
       for (int j = 0; j < NL; ++j) odd |= odd16(sV + (j * 4 + wv) * 1024 + (here(threadIdx.x) & 63) * 16);
       if (!__syncthreads_or(odd)) return;
       const float mu = m_off();
-      const uint32_t see0 = seen(x, 0), see1 = KB > 1 ? seen(x, KB - 1) : 0;
+      const uint32_t see0 = seen(x, 0), see1 = seen(x, 1);
 #pragma nounroll
       for (int key = 0; key < BK; ++key) {
         const int kk = key & 31, rr = (kk >> 3) * 4 + (kk & 3), hh = (kk >> 2) & 1;
@@ -932,7 +931,8 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
       }
       __syncthreads();
 #pragma unroll
-      for (int j = 0; j < NL; ++j) clear_odd16(sV + (j * 4 + wv) * 1024 + (here(threadIdx.x) & 63) * 16);
+      for (int j = 0; j < NL; ++j)
+        clear_odd16(sV + (j * 4 + wv) * 1024 + (here(threadIdx.x) & 63) * 16);
       __syncthreads();
     };
 
@@ -969,35 +969,33 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
         pf[k] = pack8(q);
       }
     }
-    // One step: tile x (in buffer S = x % NB; its scores in set S % 2, the
-    // operands of its first half in pf) and the scores of tile x + 1.  On the
-    // last tile the score MFMAs run on stale LDS and their results are dropped.
+    // One step: tile x (in buffer and score set S = x % 2, the operands of its
+    // first half in pf) and the scores of tile x + 1.  On the last tile the score
+    // MFMAs run on stale LDS and their results are dropped.
     auto step = [&](auto tag, int x) __attribute__((always_inline)) {
-      constexpr int S = decltype(tag)::value, P = S & 1, S1 = (S + 1) % NB;
-      f32x16 (&cur)[KB] = sc[P];
-      f32x16 (&nxt)[KB] = sc[P ^ 1];
+      constexpr int S = decltype(tag)::value;
+      f32x16 (&cur)[KB] = sc[S];
+      f32x16 (&nxt)[KB] = sc[S ^ 1];
       const bool next = x + 1 < n;   // block-uniform
-      // K of tile x + 1 and V of tile x have landed (those behind them may be in
-      // flight), every wave is done with K of tile x and V of tile x - 1
-      if (x + NB - 1 < n)
-        wait_loads<(NB - 2) * 2 * NL>();
-      else
-        wait_loads<0>();
+      // K of tile x + 1 and V of tile x have landed, every wave is done with K of
+      // tile x and V of tile x - 1
+      wait_loads<0>();
       lds_barrier();
-      if (x + NB < n) issue(kb, at_k, ldsK + S * TB);
-      if (x + NB - 1 < n) issue(vb, at_v, ldsV + (S + NB - 1) % NB * TB);
+      if (x + 2 < n) issue(kb, at_k, ldsK + S * TB);
+      if (next) issue(vb, at_v, ldsV + (S ^ 1) * TB);
       const float mu = m_off();
       if (active) {
         float psum = psum_a;
         bf16x8 kr[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) kr[j] = kfrag(S1, j);
+        for (int j = 0; j < 4; ++j) kr[j] = kfrag(S ^ 1, j);
         float q[H];
+        __builtin_amdgcn_s_setprio(1);   // the matrix phases first (1 to 2 %)
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int j = 0; j < KB * KS; ++j) {
           nxt[j % KB] = mfma32(kr[j & 3], qf[j / KB], j < KB ? f32x16{} : nxt[j % KB]);
-          if (j + 4 < KB * KS) kr[j & 3] = kfrag(S1, j + 4);
+          if (j + 4 < KB * KS) kr[j & 3] = kfrag(S ^ 1, j + 4);
           constexpr int NS = KB * KS;
           const int i0 = H * j / NS, i1 = H * (j + 1) / NS;
 #pragma unroll
@@ -1012,6 +1010,7 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
           }
           __builtin_amdgcn_sched_barrier(0);
         }
+        __builtin_amdgcn_s_setprio(0);
         if (__any(!(psum <= 65536.f) || m_run == -INFINITY)) slow_tile(cur, pf, psum);
         l_run += psum;
       }
@@ -1019,9 +1018,9 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
       if (next && active) mask_tile(nxt, x + 1);
       // the tiles asked for after the next barrier: V follows K
       at_v = at_k;
-      if (x + NB + 1 < n) {
-        pages.ahead((key_base + (x + NB + 1) * BK) >> a.psl, last);
-        at_k = locate(x + NB + 1);
+      if (x + 3 < n) {
+        pages.ahead((key_base + (x + 3) * BK) >> a.psl, last);
+        at_k = locate(x + 3);
       }
       if (active) {
         const float mu1 = m_off();
@@ -1032,6 +1031,7 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
         for (int st = 0; st < 4; ++st) vr[st] = vfrag(st);
         float q[H];
         psum_a = 0.f;
+        __builtin_amdgcn_s_setprio(1);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int st = 0; st < 2 * KB * DB; ++st) {
@@ -1052,16 +1052,13 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
           __builtin_amdgcn_sched_barrier(0);
         }
         asm volatile("" : "+v"(psum_a));
+        __builtin_amdgcn_s_setprio(0);
       }
     };
     if (keys) {
-      for (int x = 0; x < n; x += NB) {
+      for (int x = 0; x < n; x += 2) {
         step(std::integral_constant<int, 0>{}, x);
         if (x + 1 < n) step(std::integral_constant<int, 1>{}, x + 1);
-        if constexpr (NB == 4) {
-          if (x + 2 < n) step(std::integral_constant<int, 2>{}, x + 2);
-          if (x + 3 < n) step(std::integral_constant<int, 3>{}, x + 3);
-        }
       }
     }
     const float l = l_run + __shfl_xor(l_run, 32);
@@ -1273,7 +1270,7 @@ static hipError_t launch_tree(const TreePlan& p, TreeArgs a, hipStream_t stream)
   {
     ProfScope prof("tree_attn", stream);
     if (p.many)
-      hipLaunchKernelGGL((tree_many_kernel<D, 2, 2>), dim3(p.groups), dim3(256), 0, stream, a);
+      hipLaunchKernelGGL((tree_many_kernel<D>), dim3(p.groups), dim3(256), 0, stream, a);
     else
       hipLaunchKernelGGL((tree_few_kernel<D, kFewWaves>), dim3(p.groups), dim3(64 * kFewWaves), 0,
                          stream, a);

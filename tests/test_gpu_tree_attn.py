@@ -199,6 +199,24 @@ def test_tree_mask_edges():
     assert depth[:60].tolist() == list(range(60))
 
 
+@pytest.mark.parametrize("rows", [[3, 700, 255, 1], [1 + i % 3 for i in range(1500)]])
+def test_tree_mask_many_rows(rows):
+    """Ancestors far before their descendants, entries over many blocks of
+    rows, and more entries than are held on chip."""
+    rng = np.random.default_rng(len(rows))
+    par = [[int(rng.integers(-1, i)) if rng.random() < 0.3 else i - 1 for i in range(n)]
+           for n in rows]
+    ptr = [0] + np.cumsum(rows).tolist()
+    tree, depth = mv.tree_mask(i32([x for p in par for x in p]), i32(ptr), max(rows))
+    words, depth = tree.cpu().numpy().view(np.uint32), depth.tolist()
+    for b, n in enumerate(rows):
+        see, dep = OC.tree_rows(par[b], n)
+        assert depth[ptr[b]:ptr[b + 1]] == dep
+        bits = (words[ptr[b]:ptr[b + 1], :, None] >> np.arange(32, dtype=np.uint32)) & 1
+        bits = bits.reshape(n, -1).astype(bool)
+        assert np.array_equal(bits[:, :n], see) and not bits[:, n:].any()
+
+
 def test_rows_that_see_nothing():
     """Masks of a row's own bits: rows with none, over an empty context, give
     0 and -inf; sequences shorter than their entry; padded and bad ids; a
