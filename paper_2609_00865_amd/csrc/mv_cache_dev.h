@@ -116,21 +116,25 @@ __device__ __forceinline__ void store_v(u16* p, const float (&x)[V]) {
   }
 }
 
-// V consecutive pairs of one head row, starting at pair i: (x[i], x[i + P])
-// turned by the angles c, s.
+// V consecutive pairs of one head row, from pair i of P on: (x[i], x[i + P]),
+// read, and turned by the angles whose cosines and sines are c and s.
 template <int V>
-__device__ __forceinline__ void turn_pairs(const u16* x, u16* y, int i, int P, const float* c,
-                                           const float* s) {
-  float a[V], b[V], u[V], w[V];
-  load_v<V>(x + i, a);
-  load_v<V>(x + i + P, b);
-#pragma unroll
-  for (int e = 0; e < V; ++e) {
-    u[e] = a[e] * c[e] - b[e] * s[e];
-    w[e] = b[e] * c[e] + a[e] * s[e];
+struct Pairs {
+  float a[V], b[V];
+  __device__ __forceinline__ void read(const u16* x, int i, int P) {
+    load_v<V>(x + i, a);
+    load_v<V>(x + i + P, b);
   }
-  store_v<V>(y + i, u);
-  store_v<V>(y + i + P, w);
-}
+  __device__ __forceinline__ void turn(u16* y, int i, int P, const float* c, const float* s) const {
+    float u[V], w[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      u[e] = a[e] * c[e] - b[e] * s[e];
+      w[e] = b[e] * c[e] + a[e] * s[e];
+    }
+    store_v<V>(y + i, u);
+    store_v<V>(y + i + P, w);
+  }
+};
 
 }  // namespace mv

@@ -50,13 +50,30 @@ __global__ __launch_bounds__(256) void rope_axes_kernel(RopeDev r, int n, int H,
   __shared__ __align__(16) float ss[kRopeTokens * MV_ROPE_MAX_PAIRS];
   const int64_t t0 = int64_t(blockIdx.x) * nt;
   nt = int(min(int64_t(nt), n - t0));
+  const uint32_t P = r.pairs, C = P / V, total = nt * H * C;   // (a token has fewer than 2^30 elements)
+  // where a thread's pairs are: its first are read while the angles are formed
+  int t, i;
+  int64_t at_x, at_out;
+  auto place = [&](uint32_t w) {
+    const uint32_t th = w / C;
+    t = th / uint32_t(H);
+    i = int(w - th * C) * V;
+    const int64_t head = int64_t(th - t * uint32_t(H)) * d;
+    at_x = (t0 + t) * xs + head;
+    at_out = (t0 + t) * os + head;
+  };
+  Pairs<V> row;
+  if (threadIdx.x < total) {
+    place(threadIdx.x);
+    row.read(x + at_x, i, P);
+  }
   fill_angles(r, pos, n, t0, nt, sign, sc, ss);
-  const int P = r.pairs, C = P / V;
-  for (int64_t w = threadIdx.x; w < int64_t(nt) * H * C; w += 256) {
-    const int c = int(w % C), h = int(w / C % H), t = int(w / C / H);
-    const int i = c * V;
-    turn_pairs<V>(x + (t0 + t) * xs + int64_t(h) * d, out + (t0 + t) * os + int64_t(h) * d, i, P,
-                  sc + t * P + i, ss + t * P + i);
+  for (uint32_t w = threadIdx.x; w < total; w += 256) {
+    if (w != threadIdx.x) {
+      place(w);
+      row.read(x + at_x, i, P);
+    }
+    row.turn(out + at_out, i, P, sc + t * P + i, ss + t * P + i);
   }
   if (x == out) return;
   const int rest = d - 2 * P;
@@ -78,24 +95,49 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheDev a, int layer,
   __shared__ __align__(16) float ss[MV_ROPE_MAX_PAIRS];
   const int64_t t = blockIdx.x;
   const int at = slot[t];
-  if (at < 0 || (at >> a.psl) >= a.n_pages) return;   // block-uniform
   const int D = a.D, place = at & ((1 << a.psl) - 1);
+  const int CH = D / 8, P = r.pairs, C = ROPE ? P / V : CH;
+  const int kw = a.Hkv * C, vw = a.Hkv * CH;
+  // what a thread moves first is read while the slot and the angles are on their way
+  Pairs<V> row;
+  uint4 k0, v0;
+  auto k_at = [&](int w, int& i) {   // of thread-sized piece w: element of the row, and of its head
+    const int h = w / C;
+    i = (w - h * C) * (ROPE ? V : 8);
+    return h;
+  };
+  int ki, h = k_at(threadIdx.x, ki);
+  if (int(threadIdx.x) < kw) {
+    if (ROPE)
+      row.read(k + t * ks + int64_t(h) * D, ki, P);
+    else
+      k0 = ld16(k + t * ks + int64_t(h) * D + ki);
+  }
+  if (int(threadIdx.x) < vw) v0 = ld16(v + t * vs + int64_t(threadIdx.x) * 8);
+  if (ROPE) fill_angles(r, pos, n, t, 1, 1.f, sc, ss);
+  if (at < 0 || (at >> a.psl) >= a.n_pages) return;   // block-uniform
   // element offset of head 0's row; heads lie page_size rows apart
   const int64_t base = (((int64_t(layer) * a.n_pages + (at >> a.psl)) * a.Hkv << a.psl) + place) * D;
   const int64_t hs = int64_t(D) << a.psl;
-  const int CH = D / 8;
-  for (int w = threadIdx.x; w < a.Hkv * CH; w += 256) {
-    const int h = w / CH, c = w - h * CH;
-    st16(a.v + base + h * hs + c * 8, ld16(v + t * vs + int64_t(h) * D + c * 8));
-    if (!ROPE) st16(a.k + base + h * hs + c * 8, ld16(k + t * ks + int64_t(h) * D + c * 8));
+  for (int w = threadIdx.x; w < vw; w += 256) {
+    const int h = w / CH;
+    if (w != int(threadIdx.x)) v0 = ld16(v + t * vs + int64_t(w) * 8);
+    st16(a.v + base + h * hs + (w - h * CH) * 8, v0);
+  }
+  for (int w = threadIdx.x; w < kw; w += 256) {
+    if (w != int(threadIdx.x)) {
+      h = k_at(w, ki);
+      if (ROPE)
+        row.read(k + t * ks + int64_t(h) * D, ki, P);
+      else
+        k0 = ld16(k + t * ks + int64_t(h) * D + ki);
+    }
+    if (ROPE)
+      row.turn(a.k + base + h * hs, ki, P, sc + ki, ss + ki);
+    else
+      st16(a.k + base + h * hs + ki, k0);
   }
   if (!ROPE) return;
-  fill_angles(r, pos, n, t, 1, 1.f, sc, ss);
-  const int P = r.pairs, C = P / V;
-  for (int w = threadIdx.x; w < a.Hkv * C; w += 256) {
-    const int h = w / C, i = (w - h * C) * V;
-    turn_pairs<V>(k + t * ks + int64_t(h) * D, a.k + base + h * hs, i, P, sc + i, ss + i);
-  }
   const int rest = D - 2 * P;
   for (int w = threadIdx.x; w < a.Hkv * rest; w += 256) {
     const int h = w / rest, e = 2 * P + w - h * rest;
