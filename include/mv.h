@@ -763,8 +763,8 @@ mv_status mv_cache_free(const mv_cache_shape* shape, const mv_cache* cache, int3
  * rows from row_ptr[n_batch] on are left as they were.
  * A sequence may occur in several entries.  An entry that mv_cache_reserve
  * refused has no new rows to attend from.  Deterministic: the same call gives
- * the same bits.  At most MV_CACHE_MAX_SEQS entries, and some 7 million (row,
- * query head) pairs per KV head.
+ * the same bits.  At most MV_CACHE_MAX_SEQS entries, some 7 million (row,
+ * query head) pairs per KV head, and 2^28 in all.
  * ------------------------------------------------------------------------ */
 typedef struct {
   int32_t n_batch, n_rows, n_heads_q;

@@ -77,9 +77,9 @@ __device__ __forceinline__ void entries_of(const int* pre, int n, const int (&q)
 }
 
 // Deals the lowest `need` free pages to the n entries that pre divides:
-// take(q, entry, page) for q = 0, 1, ...; returns how many there were (at most need).  Every thread of the block
-// calls it; the hint is moved past the last page dealt.  (What take() stores
-// is not waited for.)
+// take(q, entry, page) for q = 0, 1, ...; returns how many there were (at most
+// need).  Every thread of the block calls it; the hint is moved past the last
+// page dealt.  (What take() stores is not waited for.)
 template <typename F>
 __device__ __forceinline__ int deal_pages(const CacheDev& a, const int* pre, int n, int need,
                                           const Search& from, int* tmp, F take) {
@@ -161,7 +161,7 @@ __global__ __launch_bounds__(kPlan) void cache_reserve_kernel(CacheDev a, int n,
   const int tid = threadIdx.x;
   const GrowIn in = n > 0 ? GrowIn(a, ids, ptr, min(tid, n - 1)) : GrowIn{};
   const Search from(a);
-  for (int t = tid; t < n_new; t += kPlan) {
+  for (int64_t t = tid; t < n_new; t += kPlan) {
     slot[t] = -1;
     if (pos) pos[t] = -1;
   }

@@ -23,8 +23,8 @@ static RopeDev rope_dev(const mv_rope_axes_spec& s) {
 }
 
 // cos and sin of tokens [t0, t0 + nt) and every pair into LDS rows of P floats
-__device__ __forceinline__ void fill_angles(const RopeDev& r, const int32_t* pos, int64_t n, int64_t t0,
-                                            int nt, float sign, float* sc, float* ss) {
+__device__ __forceinline__ void fill_angles(const RopeDev& r, const int32_t* pos, int64_t n,
+                                            int64_t t0, int nt, float sign, float* sc, float* ss) {
   const int P = r.pairs;
   for (int x = threadIdx.x; x < nt * P; x += blockDim.x) {
     const int t = x / P, i = x - t * P;
@@ -38,18 +38,19 @@ __device__ __forceinline__ void fill_angles(const RopeDev& r, const int32_t* pos
 }
 
 constexpr int kRopeTokens = 4;   // tokens of a block, at most
+constexpr int kSlice = 1 << 23;   // tokens of a launch, at most: a launch has 2^32 threads
 
 // One block per nt tokens; a thread per (token, head, V pairs), then the
 // elements that pass through.
 template <int V>
-__global__ __launch_bounds__(256) void rope_axes_kernel(RopeDev r, int n, int H, int d, int nt,
-                                                        const u16* x, int64_t xs,
+__global__ __launch_bounds__(256) void rope_axes_kernel(RopeDev r, int n, int tokens, int H, int d,
+                                                        int nt, const u16* x, int64_t xs,
                                                         const int32_t* __restrict__ pos,
                                                         float sign, u16* out, int64_t os) {
   __shared__ __align__(16) float sc[kRopeTokens * MV_ROPE_MAX_PAIRS];
   __shared__ __align__(16) float ss[kRopeTokens * MV_ROPE_MAX_PAIRS];
   const int64_t t0 = int64_t(blockIdx.x) * nt;
-  nt = int(min(int64_t(nt), n - t0));
+  nt = int(min(int64_t(nt), tokens - t0));
   const uint32_t P = r.pairs, C = P / V, total = nt * H * C;   // (a token has fewer than 2^30 elements)
   // where a thread's pairs are: its first are read while the angles are formed
   int t, i;
@@ -155,21 +156,24 @@ hipError_t launch_rope_axes(const mv_rope_axes_spec& spec, int n, int H, int d, 
   const RopeDev r = rope_dev(spec);
   // Four tokens to a block where that still leaves several blocks per CU
   const int nt = n >= kRopeTokens * 4 * kNumCu ? kRopeTokens : 1;
-  const dim3 grid(unsigned((n + nt - 1) / nt)), block(256);
   const float sign = direction > 0 ? 1.f : -1.f;
   const u16* xp = static_cast<const u16*>(x);
   u16* op = static_cast<u16*>(out);
   ProfScope prof("rope_axes", stream);
-#define MV_ROPE(V) \
-  hipLaunchKernelGGL((rope_axes_kernel<V>), grid, block, 0, stream, r, n, H, d, nt, xp, xs, pos, \
-                     sign, op, os)
-  switch (pair_width(r.pairs)) {
-    case 8: MV_ROPE(8); break;
-    case 4: MV_ROPE(4); break;
-    case 2: MV_ROPE(2); break;
-    default: MV_ROPE(1); break;
-  }
+  for (int64_t first = 0; first < n; first += kSlice) {
+    const int tokens = int(std::min(int64_t(kSlice), n - first));
+    const dim3 grid(unsigned((tokens + nt - 1) / nt)), block(256);
+#define MV_ROPE(V)                                                                           \
+  hipLaunchKernelGGL((rope_axes_kernel<V>), grid, block, 0, stream, r, n, tokens, H, d, nt, \
+                     xp + first * xs, xs, pos + first, sign, op + first * os, os)
+    switch (pair_width(r.pairs)) {
+      case 8: MV_ROPE(8); break;
+      case 4: MV_ROPE(4); break;
+      case 2: MV_ROPE(2); break;
+      default: MV_ROPE(1); break;
+    }
 #undef MV_ROPE
+  }
   return hipGetLastError();
 }
 
@@ -179,24 +183,26 @@ hipError_t launch_cache_write(const CacheDev& a, int layer, int n, const int32_t
                               hipStream_t stream) {
   RopeDev r{};
   if (spec) r = rope_dev(*spec);
-  const dim3 grid(n), block(256);
   const u16* kp = static_cast<const u16*>(k);
   const u16* vp = static_cast<const u16*>(v);
   ProfScope prof("cache_write", stream);
-#define MV_WRITE(V, ROPE) \
-  hipLaunchKernelGGL((cache_write_kernel<V, ROPE>), grid, block, 0, stream, a, layer, r, n, slot, \
-                     kp, ks, vp, vs, pos)
-  if (!spec) {
-    MV_WRITE(8, false);
-  } else {
-    switch (pair_width(r.pairs)) {
-      case 8: MV_WRITE(8, true); break;
-      case 4: MV_WRITE(4, true); break;
-      case 2: MV_WRITE(2, true); break;
-      default: MV_WRITE(1, true); break;
+  for (int64_t first = 0; first < n; first += kSlice) {
+    const dim3 grid(unsigned(std::min(int64_t(kSlice), n - first))), block(256);
+#define MV_WRITE(V, ROPE)                                                                      \
+  hipLaunchKernelGGL((cache_write_kernel<V, ROPE>), grid, block, 0, stream, a, layer, r, n,    \
+                     slot + first, kp + first * ks, ks, vp + first * vs, vs, ROPE ? pos + first : pos)
+    if (!spec) {
+      MV_WRITE(8, false);
+    } else {
+      switch (pair_width(r.pairs)) {
+        case 8: MV_WRITE(8, true); break;
+        case 4: MV_WRITE(4, true); break;
+        case 2: MV_WRITE(2, true); break;
+        default: MV_WRITE(1, true); break;
+      }
     }
-  }
 #undef MV_WRITE
+  }
   return hipGetLastError();
 }
 

@@ -1098,10 +1098,18 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
   }
 }
 
+// Whether a record can be one (if row_ptr is not as it should be, some are not
+// written): all it names lies inside the arrays.
+template <int R>
+__device__ __forceinline__ bool sound(const TreeArgs& a, const TreeJoin& j) {
+  return j.rows <= R && j.run >= 0 && j.runs >= 0 && int64_t(j.run) + j.runs <= a.groups &&
+         unsigned(j.slot) < 2u * unsigned(a.groups) && j.m0 >= 0 && j.m0 <= INT32_MAX - R &&
+         j.r0 >= 0 && int64_t(j.r0) + by_heads(a, j.m0 + j.rows - 1) < a.N;
+}
+
 // --------------------------------------------------------------------------
 // Joins the segments of a tile, in their order: block (tile place, KV head,
-// RG pairs), JG
-// groups of D / 8 threads to a pair, each for every JG-th segment.
+// RG pairs), JG groups of D / 8 threads to a pair, each for every JG-th segment.
 // --------------------------------------------------------------------------
 template <int D, int R, int JG>
 __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
@@ -1110,7 +1118,7 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
   const int rg = blockIdx.x % NG;
   const TreeJoin jn = a.join[blockIdx.x / NG];
   const int hk = blockIdx.x / NG % a.Hkv;
-  if (rg * RG >= jn.rows) return;   // block-uniform
+  if (rg * RG >= jn.rows || !sound<R>(a, jn)) return;   // block-uniform
   const int d0 = (threadIdx.x % TD) * 8, rr = threadIdx.x / TD % RG, jg = threadIdx.x / (TD * RG);
   const int r = rg * RG + rr;
   float M = -INFINITY, l = 0.f, y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -1186,8 +1194,9 @@ __global__ __launch_bounds__(256) void tree_mask_kernel(int B, int N, const int3
                                                         const int32_t* __restrict__ parent, int W,
                                                         uint32_t* __restrict__ tree,
                                                         int32_t* __restrict__ depth) {
-  const int t = blockIdx.x * 256 + threadIdx.x;
-  if (t >= min(N, ptr[B])) return;
+  const int64_t place = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  if (place >= min(N, ptr[B])) return;
+  const int t = int(place);
   int lo = 0, hi = B;   // the entry: the last with ptr <= t
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
@@ -1259,10 +1268,11 @@ size_t tree_attn_ws_bytes(const mv_cache_shape& c, const mv_tree_attn_shape& s) 
          sizeof(TreeJoin) * size_t(tiles) * c.n_heads_kv;
 }
 
-// Tile places past which the deal does not fit its LDS
+// Whether the deal fits its LDS and the join a launch (2^32 threads)
 bool tree_attn_fits(const mv_cache_shape& c, const mv_tree_attn_shape& s) {
   const TreePlan p = tree_plan(c, s);
-  return p.tiles <= kChunks * (p.many ? 256 : 64 * kFewWaves);
+  return p.tiles <= kChunks * (p.many ? 256 : 64 * kFewWaves) &&
+         int64_t(p.tiles) * c.n_heads_kv * (p.R * c.head_dim / 2048) < (int64_t(1) << 24);
 }
 
 template <int D>
@@ -1343,7 +1353,7 @@ hipError_t launch_tree_attn(const mv_cache_shape& cs, const CacheDev& cd, int la
 hipError_t launch_tree_mask(int B, int N, const int32_t* ptr, const int32_t* parent, int words,
                             uint32_t* tree, int32_t* depth, hipStream_t stream) {
   ProfScope prof("tree_mask", stream);
-  hipLaunchKernelGGL(tree_mask_kernel, dim3((N + 255) / 256), dim3(256), 0, stream, B, N, ptr,
+  hipLaunchKernelGGL(tree_mask_kernel, dim3(unsigned((int64_t(N) + 255) / 256)), dim3(256), 0, stream, B, N, ptr,
                      parent, words, tree, depth);
   return hipGetLastError();
 }

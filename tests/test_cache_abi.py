@@ -135,6 +135,15 @@ def test_tree_attn():
     assert m(ptr=None) == "MV_ERR_INVALID_ARG" and m(N=0) == "MV_OK"
 
 
+def test_more_pairs_than_a_launch_joins():
+    """2^28 pairs of a row and a query head are refused, whichever way they come."""
+    for heads, hq, rows in ((64, 64, 1 << 22), (32, 128, 1 << 21), (2, 4, 1 << 26)):
+        t = mv.TreeAttnShape(1, rows, hq, 0, 0, 0.0)
+        assert mv.mv_tree_attn_workspace_bytes(R(shape(heads=heads)), R(t)) == 0
+    t = mv.TreeAttnShape(1, 1 << 20, 64, 0, 0, 0.0)
+    assert mv.mv_tree_attn_workspace_bytes(R(shape(heads=64)), R(t)) > 0
+
+
 def test_workspace_grows_with_the_call():
     """A workspace sized for some rows and entries serves any fewer."""
     s = shape(heads=4)

@@ -245,6 +245,22 @@ def test_write_rotated_and_strided():
         p.same()
 
 
+def test_more_rows_than_a_launch_has():
+    n, spec = (1 << 23) + 3, mv.RopeAxes(64, [0] * 32)
+    c = mv.PagedCache(1, 1, 16, 1, 64, 1, 1)
+    rows = torch.tensor([0, 4444, (1 << 23) - 1, 1 << 23, n - 1], device="cuda")
+    slot = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    slot[rows] = torch.arange(5, dtype=torch.int32, device="cuda")
+    x = torch.zeros(n, 1, 64, dtype=BF, device="cuda")
+    x[rows] = torch.randn(5, 1, 64, generator=torch.Generator().manual_seed(2)).to(BF).cuda()
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")[None]
+    turned = mv.rope_axes(x[rows], pos[:, rows].contiguous(), spec)
+    for rope in (None, spec):
+        mv.cache_write(c, 0, slot, x, x, rope=rope, pos=pos)
+        assert torch.equal(c.k[0, 0, 0, :5], (turned if rope else x[rows])[:, 0])
+        assert torch.equal(c.v[0, 0, 0, :5], x[rows][:, 0])
+
+
 def test_refusals():
     c = mv.PagedCache(1, 8, 16, 2, 64, 4, 4)
     ids, ptr = i32([0, 1]), i32([0, 1, 2])

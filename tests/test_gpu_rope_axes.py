@@ -116,6 +116,17 @@ def test_inverse_is_the_gradient():
         assert abs(lhs - rhs) <= 2.0 ** -8 * (float((col * g.double()).abs().sum()) + abs(rhs)) + 1e-4
 
 
+def test_more_tokens_than_a_launch_has():
+    n, spec = (1 << 23) + 5, mv.RopeAxes(8, [0, 1, 0, 1])
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    x = torch.randn(n, 1, 8, generator=gen, device="cuda").to(BF)
+    pos = torch.randint(0, 999, (2, n), generator=gen, device="cuda", dtype=torch.int32)
+    y = mv.rope_axes(x, pos, spec)
+    for a, b in ((0, 70), (n // 2, n // 2 + 4097), (n - 4100, n)):
+        assert torch.equal(y[a:b], mv.rope_axes(x[a:b], pos[:, a:b].contiguous(), spec))
+    _check(y[-9:], x[-9:].cpu(), pos[:, -9:].cpu(), [0, 1, 0, 1], spec.theta, False)
+
+
 def test_refusals():
     spec = mv.RopeAxes(64, [0] * 32)
     x = torch.zeros(4, 2, 64, dtype=BF, device="cuda")
