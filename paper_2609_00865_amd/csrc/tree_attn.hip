@@ -535,6 +535,17 @@ struct Pair {
 
 // --------------------------------------------------------------------------
 // few pairs: NW waves, each with two K and two V tiles of 32 keys
+//
+// Bound by the reading of K and V; a wave has a tile's 16 KiB (head_dim 128) in
+// flight while it works on another.  64 single tokens over 257 to 16384 rows,
+// 28/4 heads of 128: 522 MB in 100 us, 5.2 TB/s; 6 over 65536 to 131071 rows,
+// 64/8 heads: 2.47 GB in 415 us, 5.9 TB/s.  One token over 777 rows is a chain
+// of waits, 8.5 us: about 0.5 us for the lengths, 0.7 for the deal and 0.7 for
+// finding the run in it, 1.0 for page ids, 0.9 for the first keys, 1.1 for a
+// tile and 0.9 for the waves' joint result; the launch is the rest.
+// Two waves to a workgroup and two workgroups to a CU (us: 101 and 413; four
+// waves and one workgroup 102 and 413, short runs 0 to 8 % slower; one wave and
+// four workgroups 128 and 488).  64 or 128 pairs to a wave were no faster.
 // --------------------------------------------------------------------------
 template <int D, int NW>
 __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
@@ -758,7 +769,16 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
 
 // --------------------------------------------------------------------------
 // many pairs: four waves of 32 pairs on shared tiles of 64 keys, K and V in two
-// buffers each
+// buffers each, two workgroups to a CU
+//
+// Where contexts are read once (24 trees of 8 to 61 tokens over 301 to 8192
+// rows, 28/4 heads of 128: 177 MB of keys and Q, 30 MB of partial results, 42
+// us, 4.9 TB/s) it is bound by memory; where rows are many (two chunks of 1531
+// to 2048 rows over 4099 to 8192, 420 GFLOP: 410 to 470 us with the chip's clock,
+// 0.9 to 1.0 PFLOP/s) by the matrix pipe, 58 % busy, and the six vector
+// instructions beside each MFMA that share its SIMD.  32-key tiles in four
+// buffers were 4 % slower on the chunks and 7 % at head_dim 64, up to 10 %
+// faster where runs are a few units; eight waves on 256 pairs were slower.
 // --------------------------------------------------------------------------
 template <int D>
 __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
@@ -1110,6 +1130,8 @@ __device__ __forceinline__ bool sound(const TreeArgs& a, const TreeJoin& j) {
 // --------------------------------------------------------------------------
 // Joins the segments of a tile, in their order: block (tile place, KV head,
 // RG pairs), JG groups of D / 8 threads to a pair, each for every JG-th segment.
+// Bound by the read of the partial results (the chunks above: 65 MB read, 17 MB
+// written in 13 us, 6 TB/s), or by its two dependent reads (one token: 3.2 us).
 // --------------------------------------------------------------------------
 template <int D, int R, int JG>
 __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
@@ -1189,7 +1211,9 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a) {
     a.lse[int64_t(pr.h) * a.N + pr.row] = lse_of(M, l);
 }
 
-// A thread to a row: up the parents, its words from the highest down.
+// A thread to a row: up the parents, its words from the highest down.  Latency:
+// 24 trees of 8 to 61 tokens 4.6 us, 9 of 5 to 33 3.1.  (The parents held in LDS
+// for the walk made no difference.)
 __global__ __launch_bounds__(256) void tree_mask_kernel(int B, int N, const int32_t* __restrict__ ptr,
                                                         const int32_t* __restrict__ parent, int W,
                                                         uint32_t* __restrict__ tree,
