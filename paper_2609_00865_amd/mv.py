@@ -850,7 +850,8 @@ def rope_axes(x, pos, rope: RopeAxes, inverse: bool = False, out=None, stream=No
     n, heads, d = shape
     _rope_pos(rope, pos, n)
     if out is None:
-        out = torch.empty(shape, dtype=torch.bfloat16, device=x.device)
+        out = (torch.empty_like(x) if x.is_contiguous()
+               else torch.empty(shape, dtype=torch.bfloat16, device=x.device))
         handle, out_stride = _use(stream, out), heads * d
     else:
         _need(out, torch.bfloat16, "out", shape, contiguous=False)
@@ -947,7 +948,7 @@ def cache_reserve(cache: PagedCache, seq_ids, new_ptr, n_new: int, stream=None):
     _need_ids(new_ptr, "new_ptr", seq_ids.numel() + 1)
     dev = seq_ids.device
     slot = torch.empty(int(n_new), dtype=torch.int32, device=dev)
-    pos = torch.empty(int(n_new), dtype=torch.int32, device=dev)
+    pos = torch.empty_like(slot)
     check(mv_cache_reserve(*cache._args(), seq_ids.numel(), _ptr(seq_ids), _ptr(new_ptr),
                            int(n_new), _ptr(slot), _ptr(pos), _use(stream, slot, pos)))
     return slot, pos
@@ -1023,7 +1024,7 @@ def tree_mask(parent, row_ptr, max_rows: int, stream=None):
         raise ValueError("row_ptr: expected n_batch + 1 entries")
     n, words = parent.numel(), max(1, (int(max_rows) + 31) // 32)
     tree = torch.empty((n, words), dtype=torch.int32, device=parent.device)
-    depth = torch.empty(n, dtype=torch.int32, device=parent.device)
+    depth = torch.empty_like(parent)
     check(mv_tree_mask(row_ptr.numel() - 1, n, _ptr(row_ptr), _ptr(parent), words, _ptr(tree),
                        _ptr(depth), _use(stream, tree, depth)))
     return tree, depth
