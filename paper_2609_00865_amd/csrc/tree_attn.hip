@@ -1313,21 +1313,26 @@ static hipError_t launch_tree(const TreePlan& p, TreeArgs a, hipStream_t stream)
   // one workgroup's run is every tile
   if (p.groups == 1) return hipSuccess;
   ProfScope prof("tree_combine", stream);
-  // The more segments a tile may have, the more groups of threads share a pair's
-  // (one sequence of 8000 keys, 125 segments a tile: 15 us by four groups, less
-  // by sixteen); where there are few, blocks of more pairs do it sooner.
+  // The more segments a tile has on average, the more groups of threads share a
+  // pair's, which otherwise wait for one after another (us by one, four and
+  // sixteen groups: 9 trees, 17 segments a tile, - / 10.2 / 7.4; 16 trees, 5
+  // segments, 10.4 / 7.5 / -); with fewer segments than threads to read them the
+  // blocks are only smaller (8 trees, 8 segments, - / 8.5 / 10.8; 24 trees of 64
+  // tokens, 3 segments, 12.6 / 16.7 / -).  Tiles of 32 pairs are single tokens',
+  // whose long ones have many more than the average (64 tokens over 257 to 16384
+  // rows, 2 segments, 8.4 / 7.1 / -).
   const int64_t segments = p.groups / (int64_t(p.tiles) * a.Hkv);
 #define MV_JOIN(R, JG)                                                                         \
   hipLaunchKernelGGL((tree_join_kernel<D, R, JG>),                                             \
                      dim3(unsigned(p.tiles * a.Hkv * (R * JG * D / 2048))), dim3(256), 0, stream, \
                      a)
   if (p.many) {
-    if (segments >= 32) MV_JOIN(128, 16);
-    else if (segments >= 8) MV_JOIN(128, 4);
+    if (segments >= 16) MV_JOIN(128, 16);
+    else if (segments >= 4) MV_JOIN(128, 4);
     else MV_JOIN(128, 1);
   } else {
-    if (segments >= 32) MV_JOIN(32, 16);
-    else if (segments >= 8) MV_JOIN(32, 4);
+    if (segments >= 16) MV_JOIN(32, 16);
+    else if (segments >= 1) MV_JOIN(32, 4);
     else MV_JOIN(32, 1);
   }
 #undef MV_JOIN
