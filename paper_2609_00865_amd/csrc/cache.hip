@@ -11,10 +11,10 @@
 // order of their atomics does not show.
 //
 // The move is bound by memory (16 spans out of 32768 rows of 8 layers, 4 heads
-// of 128: 620 MB in 121 us, 5.1 TB/s), the others are chains of dependent reads
-// and barriers: reserve 6.8 us (16 sequences), plan 7.0 (32 forks) and 6.6 (the
-// edit above), release 4.6 (32 sequences) and 7.2 (one of 2048 pages), move 5.3
-// (the part-filled pages of 32 forks).
+// of 128: 620 MB in 127 us, 4.9 TB/s, a large copy's rate), the others are
+// chains of dependent reads and barriers: reserve 6.8 us (16 sequences), plan 7.1
+// (32 forks) and 5.1 (the edit above), release 4.8 (32 sequences) and 7.1 (one of
+// 2048 pages), move 5.2 (the part-filled pages of 32 forks).
 #include "mv_cache_dev.h"
 
 namespace mv {

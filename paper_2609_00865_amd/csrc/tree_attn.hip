@@ -772,8 +772,8 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
 // buffers each, two workgroups to a CU
 //
 // Where contexts are read once (24 trees of 8 to 61 tokens over 301 to 8192
-// rows, 28/4 heads of 128: 177 MB of keys and Q, 30 MB of partial results, 42
-// us, 4.9 TB/s) it is bound by memory; where rows are many (two chunks of 1531
+// rows, 28/4 heads of 128: 181 MB of keys and Q, 30 MB of partial results, 42
+// us, 5.0 TB/s) it is bound by memory; where rows are many (two chunks of 1531
 // to 2048 rows over 4099 to 8192, 420 GFLOP: 410 to 470 us with the chip's clock,
 // 0.9 to 1.0 PFLOP/s) by the matrix pipe, 58 % busy, and the six vector
 // instructions beside each MFMA that share its SIMD.  32-key tiles in four
