@@ -1023,7 +1023,7 @@ def tree_mask(parent, row_ptr, max_rows: int, stream=None):
     if row_ptr.numel() < 1:
         raise ValueError("row_ptr: expected n_batch + 1 entries")
     n, words = parent.numel(), max(1, (int(max_rows) + 31) // 32)
-    tree = torch.empty((n, words), dtype=torch.int32, device=parent.device)
+    tree = torch.empty(n, words, dtype=torch.int32, device=parent.device)
     depth = torch.empty_like(parent)
     check(mv_tree_mask(row_ptr.numel() - 1, n, _ptr(row_ptr), _ptr(parent), words, _ptr(tree),
                        _ptr(depth), _use(stream, tree, depth)))
@@ -1067,7 +1067,7 @@ def tree_attn(cache: PagedCache, layer: int, q, seq_ids, row_ptr, tree=None,
     refs, dev = cache._args(), q.device
     if out is None:
         o = torch.empty_like(q)
-        lse = torch.empty((heads, n), dtype=torch.float32, device=dev)
+        lse = torch.empty(heads, n, dtype=torch.float32, device=dev)
     else:
         o, lse = out
         _need(o, torch.bfloat16, "o", dims)
