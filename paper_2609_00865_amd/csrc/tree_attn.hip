@@ -13,7 +13,8 @@
 // Two kernels take a segment.  For few pairs (tree_few_kernel, R = 32) the
 // time is the reading of K and V: each wave streams 32-key tiles of its own
 // through its own LDS buffers, no barrier between waves, and the waves'
-// results meet in LDS at the end.  For many pairs (tree_many_kernel, R = 128)
+// results meet in LDS at the end.  (Few pairs of sequences known not to be long
+// are not dealt: a workgroup takes a tile whole.)  For many pairs (tree_many_kernel, R = 128)
 // the products count: four waves of 32 pairs share 64-key tiles, and the
 // scores of a tile are computed while the vector ALU turns those of the one
 // before into probabilities.  Both compute S^T = K Q^T and O^T += V^T P^T with
@@ -366,6 +367,68 @@ struct Deal {
   }
 };
 
+// Instead of a deal: a workgroup to a tile place and KV head, all of the tile's
+// keys, no partial results.
+struct WholeShared {
+  Tile tile;
+  int id, first;
+};
+
+template <int R, int BLOCK>
+struct Whole {
+  const TreeArgs& a;
+  Tile t;
+  int hk, unit, n, id;
+  bool over;
+
+  __device__ __forceinline__ Whole(const TreeArgs& args, WholeShared& s) : a(args), unit(0), over(true) {
+    const int u = blockIdx.x / a.Hkv;
+    hk = blockIdx.x - u * a.Hkv;
+    if (threadIdx.x == 0) s.first = INT32_MAX;
+    lds_barrier();
+    // Each thread looks at entries of its own: the place is in one of them (if
+    // row_ptr is not as it should be, in the first)
+    int b = INT32_MAX, my_id = -1;
+    Tile mine{};
+    for (int e = threadIdx.x; e < a.B; e += BLOCK) {
+      const int r0 = min(max(a.ptr[e], 0), a.N), r1 = min(max(a.ptr[e + 1], 0), a.N);
+      const int e_id = a.ids[e];
+      const int64_t m0 = int64_t(u - first_place<R>(r0, e, a.G)) * R;
+      if (b != INT32_MAX || r1 <= r0 || m0 < 0 || m0 >= int64_t(r1 - r0) * a.G) continue;
+      b = e;
+      my_id = e_id;
+      mine.b = e;
+      mine.r0 = r0;
+      mine.n = r1 - r0;
+      mine.m0 = int(m0);
+      mine.rows = min(R, mine.n * a.G - mine.m0);
+      const int L = entry_len(a, e_id);
+      mine.c = L - mine.n;
+      mine.kmax = a.tree ? L : max(0, mine.c + by_heads(a, mine.m0 + mine.rows - 1) + 1);
+      atomicMin(&s.first, e);
+    }
+    lds_barrier();
+    if (s.first == INT32_MAX) return;   // block-uniform: no tile
+    if (b == s.first) {
+      s.tile = mine;
+      s.id = my_id;
+    }
+    lds_barrier();
+    t = uniform(s.tile);
+    id = uniform(s.id);
+    n = t.units();
+    over = false;
+  }
+  __device__ __forceinline__ bool done() const { return over; }
+  __device__ __forceinline__ void next() { over = true; }
+  __device__ __forceinline__ bool whole() const { return true; }
+  __device__ __forceinline__ int64_t slot() const { return 0; }
+  __device__ __forceinline__ void note() const {}
+  __device__ __forceinline__ const int32_t* pages() const {
+    return a.table + int64_t(id) * a.max_pages;
+  }
+};
+
 // Workgroups of an XCD (dealt to them in turn) take neighbouring runs: tiles
 // of one sequence and KV head meet in its L2.
 __device__ __forceinline__ int run_of_block(int groups) {
@@ -534,35 +597,44 @@ struct Pair {
 };
 
 // --------------------------------------------------------------------------
-// few pairs: NW waves, each with two K and two V tiles of 32 keys
+// few pairs: NW waves, each with two K and two V tiles of 32 keys, a run of the
+// deal; or (WHOLE) with one of each, all keys of one tile: K of a wave's next tile
+// is asked for when K of this one is used up, V likewise.
 //
 // Bound by the reading of K and V; a wave has a tile's 16 KiB (head_dim 128) in
 // flight while it works on another.  64 single tokens over 257 to 16384 rows,
 // 28/4 heads of 128: 522 MB in 100 us, 5.2 TB/s; 6 over 65536 to 131071 rows,
 // 64/8 heads: 2.47 GB in 415 us, 5.9 TB/s.  One token over 777 rows is a chain
-// of waits, 8.5 us: about 0.5 us for the lengths, 0.7 for the deal and 0.7 for
-// finding the run in it, 1.0 for page ids, 0.9 for the first keys, 1.1 for a
-// tile and 0.9 for the waves' joint result; the launch is the rest.
+// of waits: dealt 8.4 us (about 0.5 for the lengths, 0.7 for the deal and 0.7 for
+// finding the run in it, 1.0 for page ids, 0.9 for the first keys, 1.1 for a tile
+// and 0.9 for the waves' joint result, the launch the rest) and 3.4 for the join;
+// whole 11.6, of one launch.
 // Two waves to a workgroup and two workgroups to a CU (us: 101 and 413; four
 // waves and one workgroup 102 and 413, short runs 0 to 8 % slower; one wave and
 // four workgroups 128 and 488).  64 or 128 pairs to a wave were no faster.
 // --------------------------------------------------------------------------
-template <int D, int NW>
+template <int D, int NW, bool WHOLE>
 __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
-  constexpr int R = 32, BLOCK = NW * 64;
+  constexpr int R = 32, BLOCK = NW * 64, NB = WHOLE ? 1 : 2;
   constexpr int KS = D / 16, DB = D / 32;
   constexpr int TB = 32 * D * 2;             // bytes of a tile
   constexpr int NI = TB / 1024;              // 1 KiB loads of a tile
   constexpr int LR = 512 / D;                // rows of a load
-  constexpr int OS = D + 4;                  // floats of a row of O where the waves meet
-  static_assert(R * OS * 4 <= 4 * TB, "a wave's O fits its tiles");
-  __shared__ __align__(1024) char buf[NW][4 * TB];   // K, K, V, V
+  // floats of a row of O where the waves meet; its 16-byte chunks are permuted by
+  // row where there is no room to set rows apart
+  constexpr int OS = WHOLE ? D : D + 4;
+  static_assert(R * OS * 4 <= 2 * NB * TB, "a wave's O fits its tiles");
+  auto chunk_at = [](int r, int ch) { return r * OS + (WHOLE ? ch ^ (r & (D / 4 - 1)) : ch) * 4; };
+  __shared__ __align__(1024) char buf[NW][2 * NB * TB];   // K's, V's
   __shared__ __align__(16) int pg[NW][128];
-  __shared__ TreeShared sh;
+  __shared__ std::conditional_t<WHOLE, WholeShared, TreeShared> sh;
   __shared__ float sm[NW][R], sl[NW][R];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int c = lane & 31, g = lane >> 5;
-  Deal<R, BLOCK, false> deal(a, sh, run_of_block(a.groups));
+  auto deal = [&] {
+    if constexpr (WHOLE) return Whole<R, BLOCK>(a, sh);
+    else return Deal<R, BLOCK, false>(a, sh, run_of_block(a.groups));
+  }();
   const int ps = 1 << a.psl;
   // A load's LR rows lie in one page; its address is scalar but for one of
   // 16 / LR offsets per lane (the chunks' permutation has a period of 16 rows).
@@ -574,7 +646,7 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
     voff[j] = uint32_t(r * D * 2 + ((lane % (D / 8) ^ kv_swz<D>(j * LR + r)) << 4));
   }
   const int wv = uniform(wave);
-  const uint32_t lds0 = lds_addr(&buf[0][0]) + wv * 4 * TB;
+  const uint32_t lds0 = lds_addr(&buf[0][0]) + wv * 2 * NB * TB;
 
   for (; !deal.done(); deal.next()) {
     const Tile& t = deal.t;
@@ -610,37 +682,51 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
     for (int ks = 0; ks < KS; ++ks)
       qf[ks] = as_bf16x8(ld16(a.q + (mine.row * a.Hq + mine.h) * D + ks * 16 + g * 8));
     wait_loads<KS>();   // the page ids have landed, Q may be on its way
-    // Tile x of this wave into buffer x & 1.  Rows past the last key are read
+    // Tile x of this wave into buffer x % NB.  Rows past the last key are read
     // from the last key's page (what they hold is masked).
-    auto issue = [&](int x) {
+    uint32_t at;   // where 16 rows at a time are, of the tile last asked for
+    auto issue = [&](const char* base, uint32_t lds) {
+#pragma unroll
+      for (int j = 0; j < NI; ++j)
+        lds_load16s(base + int64_t(read_lane(at, j / NO)) * (D * 2) + (j % NO) * 1024, voff[j % NO],
+                    lds + j * 1024);
+    };
+    auto issue_k = [&](int x) {
       const int key0 = key_of(x);
       pages.ahead(key0 >> a.psl, last);
-      const uint32_t kl = lds0 + uint32_t(x & 1) * TB;
-      // (16 rows of a page at a time)
-      const uint32_t at = pages.row_of(key0 + (lane & 1) * 16, last, page_rows);
-#pragma unroll
-      for (int j = 0; j < NI; ++j) {
-        const int64_t x0 = int64_t(read_lane(at, j / NO)) * (D * 2) + (j % NO) * 1024;
-        lds_load16s(kb + x0, voff[j % NO], kl + j * 1024);
-        lds_load16s(vb + x0, voff[j % NO], kl + 2 * TB + j * 1024);
-      }
+      at = pages.row_of(key0 + (lane & 1) * 16, last, page_rows);
+      issue(kb, lds0 + uint32_t(x % NB) * TB);
     };
-    if (todo > 0) issue(0);
+    auto issue_v = [&](int x) { issue(vb, lds0 + uint32_t(NB + x % NB) * TB); };
+    if (todo > 0) {
+      issue_k(0);
+      issue_v(0);
+    }
     wait_loads<0>();
     settle(qf);
-    if (todo > 1) issue(1);
+    if (!WHOLE && todo > 1) {
+      issue_k(1);
+      issue_v(1);
+    }
     const int clear = a.tree ? t.c : t.c + by_heads(a, t.m0) + 1;   // keys every row of the tile sees
     for (int x = 0; x < todo; ++x) {
-      // the tile has landed (the next one's loads may be in flight)
-      if (x + 1 < todo)
+      // K of the tile has landed, and with two buffers V too (behind them may be
+      // in flight: V; the next tile)
+      if (WHOLE)
+        wait_loads<NI>();
+      else if (x + 1 < todo)
         wait_loads<2 * NI>();
       else
         wait_loads<0>();
-      const char* sK = &buf[wave][(x & 1) * TB];
-      char* sV = &buf[wave][(x & 1) * TB + 2 * TB];
+      const char* sK = &buf[wave][(x % NB) * TB];
+      char* sV = &buf[wave][(NB + x % NB) * TB];
       f32x16 sc = {};
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) sc = mfma32(ld_row_swz<D>(sK, c, ks * 2 + g), qf[ks], sc);
+      if (WHOLE && x + 1 < todo) {
+        wait_lds();   // K's reads are done
+        issue_k(x + 1);
+      }
       const int key0 = key_of(x);
       uint32_t see = ~0u;
       const bool masked = key0 + 32 > min(clear, k_end);   // wave-uniform
@@ -675,6 +761,12 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
         part[r & 3] += sc[r];
       }
       l_run += (part[0] + part[1]) + (part[2] + part[3]);
+      if (WHOLE) {   // V has landed (the next K may be in flight)
+        if (x + 1 < todo)
+          wait_loads<NI>();
+        else
+          wait_loads<0>();
+      }
       if (masked) {
         // A value that is not finite in a row that some query does not see
         // would reach it as 0 * inf: such elements are taken out of the tile
@@ -703,9 +795,10 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
       for (int st = 0; st < 2 * DB; ++st)
         oacc[st % DB] = mfma32(ld_tr_swz<D>(sV, (st / DB) * 16, (st % DB) * 32), pf[st / DB],
                                oacc[st % DB]);
-      if (x + 2 < todo) {
+      if (x + NB < todo) {
         wait_lds();   // the buffer's reads are done
-        issue(x + 2);
+        if (!WHOLE) issue_k(x + NB);
+        issue_v(x + NB);
       }
     }
     l_run += __shfl_xor(l_run, 32);
@@ -725,7 +818,7 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
     for (int db = 0; db < DB; ++db)
 #pragma unroll
       for (int q4 = 0; q4 < 4; ++q4)
-        *reinterpret_cast<float4*>(so + c * OS + db * 32 + q4 * 8 + g * 4) =
+        *reinterpret_cast<float4*>(so + chunk_at(c, db * 8 + q4 * 2 + g)) =
             make_float4(oacc[db][q4 * 4 + 0] * f, oacc[db][q4 * 4 + 1] * f,
                         oacc[db][q4 * 4 + 2] * f, oacc[db][q4 * 4 + 3] * f);
     __syncthreads();
@@ -740,9 +833,9 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
       float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int w = 0; w < NW; ++w) {
-        const float* q = reinterpret_cast<const float*>(&buf[w][0]) + r * OS + d0;
+        const float* q = reinterpret_cast<const float*>(&buf[w][0]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] += q[e];
+        for (int e = 0; e < 8; ++e) y[e] += q[chunk_at(r, d0 / 4 + e / 4) + e % 4];
       }
       if (deal.whole()) {
         const Pair pr(a, t, hk, t.m0 + r);
@@ -1251,12 +1344,21 @@ __global__ __launch_bounds__(256) void tree_mask_kernel(int B, int N, const int3
 // --------------------------------------------------------------------------
 // launches
 // --------------------------------------------------------------------------
-constexpr int kFewWaves = 2;
+constexpr int kFewWaves = 2, kWholeWaves = 8;
+// Few pairs, sequences known not to be long and no more tiles than two to a CU:
+// whole tiles by eight waves each, one launch in place of two and no deal.  A
+// round of 256 keys takes 1.15 us, so where single tiles leave the chip idle the
+// deal's splitting wins from some 1600 keys on, where they fill a good part of it
+// later (us, whole / dealt and joined, 28/4 heads of 128: 1 sequence of 1024
+// keys 14.5 / 16.2, of 2048 19.3 / 16.6; 16 of 1024 15.6 / 27.3, of 4096 32.9 /
+// 37.0, of 512 to 4096 30.4 / 29.6; 32 of 512 to 4096 33.6 / 37.0; 64 of 1024
+// 35.2 / 37.8, of 2048 60.7 / 56.0; 128 of 512 39.2 / 41.4, 256 of 64 39.9 / 35.0).
+constexpr int kWholeLen = 1536, kWholeLenMid = 4096;
 // Pairs per entry up to which the kernel for few pairs is used
 constexpr int kFewPairs = 32;
 
 struct TreePlan {
-  bool many;
+  bool many, whole;
   int R, tiles, groups;
   size_t o_bytes, ml_bytes, bytes;
 };
@@ -1276,6 +1378,10 @@ static TreePlan tree_plan(const mv_cache_shape& c, const mv_tree_attn_shape& s) 
   p.many = pairs > int64_t(kFewPairs) * s.n_batch;
   p.R = p.many ? 128 : 32;
   p.tiles = int(pairs / p.R) + s.n_batch;
+  const int64_t whole = int64_t(p.tiles) * c.n_heads_kv;   // workgroups, if so
+  const bool mid = whole >= kNumCu / 4 && whole < kNumCu;
+  p.whole = !p.many && s.max_len > 0 && s.max_len <= (mid ? kWholeLenMid : kWholeLen) &&
+            whole <= 2 * kNumCu;
   p.groups = tree_groups(c, s, p.tiles);
   p.o_bytes = size_t(2 * p.groups) * p.R * c.head_dim * 4;
   p.ml_bytes = size_t(2 * p.groups) * p.R * 2 * 4;
@@ -1305,13 +1411,16 @@ static hipError_t launch_tree(const TreePlan& p, TreeArgs a, hipStream_t stream)
     ProfScope prof("tree_attn", stream);
     if (p.many)
       hipLaunchKernelGGL((tree_many_kernel<D>), dim3(p.groups), dim3(256), 0, stream, a);
+    else if (p.whole)
+      hipLaunchKernelGGL((tree_few_kernel<D, kWholeWaves, true>), dim3(p.tiles * a.Hkv),
+                         dim3(64 * kWholeWaves), 0, stream, a);
     else
-      hipLaunchKernelGGL((tree_few_kernel<D, kFewWaves>), dim3(p.groups), dim3(64 * kFewWaves), 0,
-                         stream, a);
+      hipLaunchKernelGGL((tree_few_kernel<D, kFewWaves, false>), dim3(p.groups),
+                         dim3(64 * kFewWaves), 0, stream, a);
   }
   if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  // one workgroup's run is every tile
-  if (p.groups == 1) return hipSuccess;
+  // every tile was one workgroup's
+  if (p.whole || p.groups == 1) return hipSuccess;
   ProfScope prof("tree_combine", stream);
   // The more segments a tile has on average, the more groups of threads share a
   // pair's, which otherwise wait for one after another (us by one, four and
