@@ -65,20 +65,27 @@ struct Search {
   int4 refs;
   __device__ __forceinline__ explicit Search(const CacheDev& a)
       : base(max(0, a.ctl[kCtlHint]) & ~3), refs(refs_at(a, base)) {}
+  // Waits for them: where they are used the wait would also be for every store
+  // made by then.
+  __device__ __forceinline__ void settle() {
+    asm volatile("" : "+v"(refs.x), "+v"(refs.y), "+v"(refs.z), "+v"(refs.w));
+  }
 };
 
 // The last e with pre[e] <= q, of n >= 1 ascending prefix sums (pre[0] = 0),
-// for four q at a time: their look-ups in LDS wait together.
+// for four q at a time: their look-ups in LDS are unconditional, so they wait
+// together (by themselves, a plan of 32 forks took 0.3 us longer).
 __device__ __forceinline__ void entries_of(const int* pre, int n, const int (&q)[4],
                                            int (&e)[4]) {
 #pragma unroll
   for (int u = 0; u < 4; ++u) e[u] = 0;
   for (int step = 1 << (31 - __clz(n)); step; step >>= 1) {
+    int p[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int x = e[u] + step;
-      if (x < n && pre[x] <= q[u]) e[u] = x;
-    }
+    for (int u = 0; u < 4; ++u) p[u] = pre[min(e[u] + step, n)];   // (pre[n] is the sum: past any q)
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (e[u] + step < n && p[u] <= q[u]) e[u] += step;
   }
 }
 
@@ -166,7 +173,7 @@ __global__ __launch_bounds__(kPlan) void cache_reserve_kernel(CacheDev a, int n,
   __shared__ int cnt[2], cut_e;
   const int tid = threadIdx.x;
   const GrowIn in = n > 0 ? GrowIn(a, ids, ptr, min(tid, n - 1)) : GrowIn{};
-  const Search from(a);
+  Search from(a);
   for (int64_t t = tid; t < n_new; t += kPlan) {
     slot[t] = -1;
     if (pos) pos[t] = -1;
@@ -179,6 +186,7 @@ __global__ __launch_bounds__(kPlan) void cache_reserve_kernel(CacheDev a, int n,
     if (unsigned(x) < unsigned(a.n_seqs)) atomicMin(&claim[x], e);
   }
   lds_barrier();
+  from.settle();
   int need = 0;
   for (int e0 = 0; e0 < n; e0 += kPlan) {
     const int e = e0 + tid;
@@ -344,7 +352,7 @@ __global__ __launch_bounds__(kPlan) void cache_plan_kernel(CacheDev a, int n,
   // entries read is asked for before anything waits.
   const int gs = span_ptr ? 64 : 1, lane = tid & (gs - 1);
   const MoveIn ahead(a, src, dst, span_ptr, spans, n_spans, min(tid / gs, n - 1), lane);   // (n >= 1)
-  const Search from(a);
+  Search from(a);
   for (int s = tid; s < a.n_seqs; s += kPlan) claim[s] = n;
   for (int s = tid; s < kMaxSeqs / 32; s += kPlan) inplace[s] = 0;
   if (tid == 0) cnt[0] = cnt[1] = 0, cut = INT32_MAX;
@@ -357,6 +365,7 @@ __global__ __launch_bounds__(kPlan) void cache_plan_kernel(CacheDev a, int n,
     }
   }
   lds_barrier();
+  from.settle();
   // an entry's spans, and what becomes of its pages
   const int mask = (1 << a.psl) - 1;
   for (int e = tid / gs; e < n; e += kPlan / gs) {
