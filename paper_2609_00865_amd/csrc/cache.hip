@@ -11,8 +11,8 @@
 // order of their atomics does not show.
 //
 // The move is bound by memory (16 spans out of 32768 rows of 8 layers, 4 heads
-// of 128: 620 MB in 127 us, 4.9 TB/s, a large copy's rate), the others are
-// chains of dependent reads and barriers: reserve 6.8 us (16 sequences), plan 7.1
+// of 128: 620 MB in 110 to 127 us, at or above a large copy's 4.9 TB/s), the others are
+// chains of dependent reads and barriers: reserve 6.8 us (16 sequences), plan 6.2
 // (32 forks) and 5.1 (the edit above), release 4.8 (32 sequences) and 7.1 (one of
 // 2048 pages), move 5.2 (the part-filled pages of 32 forks).
 #include "mv_cache_dev.h"
