@@ -187,8 +187,8 @@ __device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {   // of what
 // for 0 / 2 / 4 / 6 more: 4000 rows of a prompt over no context, 28/4 heads,
 // 234 / 187 / 168 / 155; 64 rollouts' decode over 257 to 16384 keys
 // 111 / 103 / 101 / 102; 128 over 250 to 1000 keys - / 37.3 / 37.9 / 41.1).
-// AGAIN: the arguments are read from where they were passed each time (the
-// kernel has no scalar registers to hold them in).
+// AGAIN: behind the constructor the arguments are read from where they were
+// passed each time (the kernel has no scalar registers to hold them in).
 constexpr int kTileCostMany = 6, kTileCostFew = 4, kLongRun = 8;
 
 template <int R, int BLOCK, bool AGAIN>
@@ -213,7 +213,7 @@ struct Deal {
 
   // The tiles of places [j BLOCK, (j + 1) BLOCK): units and tiles before each
   __device__ __forceinline__ void scan(int j, Tile& mine, int (&before)[2], int (&sum)[2]) {
-    const TreeArgs& a = args();
+    const TreeArgs& a = direct;
     const int u = j * BLOCK + threadIdx.x;
     mine = Tile{};
     if (u < a.tiles) mine = tile_of<R>(a, s, u);
@@ -246,7 +246,7 @@ struct Deal {
 
   __device__ __forceinline__ Deal(const TreeArgs& a0, TreeShared& sh, int r)
       : direct(a0), s(sh), run(r), seg(0) {
-    const TreeArgs& a = args();
+    const TreeArgs& a = direct;
     if (a.B <= kPlanB) {
       for (int b = threadIdx.x; b <= a.B; b += BLOCK) {
         s.ptr[b] = min(max(a.ptr[b], 0), a.N);
@@ -381,7 +381,8 @@ struct Whole {
   int hk, unit, n, id;
   bool over;
 
-  __device__ __forceinline__ Whole(const TreeArgs& args, WholeShared& s) : a(args), unit(0), over(true) {
+  __device__ __forceinline__ Whole(const TreeArgs& args, WholeShared& s)
+      : a(args), unit(0), over(true) {
     const int u = blockIdx.x / a.Hkv;
     hk = blockIdx.x - u * a.Hkv;
     if (threadIdx.x == 0) s.first = INT32_MAX;
