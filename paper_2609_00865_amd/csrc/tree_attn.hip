@@ -493,8 +493,8 @@ struct PageRing {
   static __device__ __forceinline__ void lds_load4(const void* src, uint32_t lds) {
     uint32_t saved;
     asm volatile(
-        "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\tglobal_load_lds_dword %1, off\n\t"
-        "s_mov_b32 m0, %0"
+        "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\t"
+        "global_load_lds_dword %1, off\n\ts_mov_b32 m0, %0"
         : "=&s"(saved)
         : "v"(src), "s"(__builtin_amdgcn_readfirstlane(lds))
         : "memory");
@@ -520,15 +520,42 @@ struct PageRing {
   }
 };
 
-// lds_load16s with an LDS address that is in a scalar register as it is
-__device__ __forceinline__ void lds_load16u(const void* base, uint32_t off, uint32_t lds) {
+// 16 rows of a page (N KiB) into LDS by direct loads of 1 KiB: lane l's 16 bytes
+// of load j from base + voff[j] + j KiB to lds + j KiB + 16 l.  The instruction's
+// offset moves both addresses, so the LDS address is set once; it is read a state
+// after it is written.
+template <int N>
+__device__ __forceinline__ void load_rows16(const void* base, const uint32_t (&voff)[N],
+                                            uint32_t lds) {
+  static_assert(N == 4 || N == 2, "rows of 128 or 64 elements");
   uint32_t saved;
-  asm volatile(
-      "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\tglobal_load_lds_dwordx4 %1, %2\n\t"
-      "s_mov_b32 m0, %0"
-      : "=&s"(saved)
-      : "v"(off), "s"(base), "s"(lds)
-      : "memory");
+  if constexpr (N == 4)
+    asm volatile(
+        "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %6\n\ts_nop 0\n\t"
+        "global_load_lds_dwordx4 %1, %5\n\tglobal_load_lds_dwordx4 %2, %5 offset:1024\n\t"
+        "global_load_lds_dwordx4 %3, %5 offset:2048\n\t"
+        "global_load_lds_dwordx4 %4, %5 offset:3072\n\ts_mov_b32 m0, %0"
+        : "=&s"(saved)
+        : "v"(voff[0]), "v"(voff[1]), "v"(voff[2]), "v"(voff[3]), "s"(base), "s"(lds)
+        : "memory");
+  else
+    asm volatile(
+        "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %4\n\ts_nop 0\n\t"
+        "global_load_lds_dwordx4 %1, %3\n\tglobal_load_lds_dwordx4 %2, %3 offset:1024\n\t"
+        "s_mov_b32 m0, %0"
+        : "=&s"(saved)
+        : "v"(voff[0]), "v"(voff[1]), "s"(base), "s"(lds)
+        : "memory");
+}
+
+// The offsets per lane of loads of 16 rows: load j's lane has chunk c ^ kv_swz of
+// its row, which repeats every 16 rows.
+template <int D>
+__device__ __forceinline__ void row_offsets(int lane, uint32_t (&voff)[D / 32]) {
+  const int r = lane / (D / 8);
+#pragma unroll
+  for (int j = 0; j < D / 32; ++j)
+    voff[j] = uint32_t(r * D * 2 + ((lane % (D / 8) ^ kv_swz<D>(j * (512 / D) + r)) << 4));
 }
 
 template <int N>
@@ -637,17 +664,11 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
     else return Deal<R, BLOCK, false>(a, sh, run_of_block(a.groups));
   }();
   const int ps = 1 << a.psl;
-  // A load's LR rows lie in one page; its address is scalar but for one of
-  // 16 / LR offsets per lane (the chunks' permutation has a period of 16 rows).
-  constexpr int NO = 16 / LR;
+  constexpr int NO = 16 / LR;                // loads of 16 rows, which lie in one page
   uint32_t voff[NO];
-#pragma unroll
-  for (int j = 0; j < NO; ++j) {
-    const int r = lane / (D / 8);
-    voff[j] = uint32_t(r * D * 2 + ((lane % (D / 8) ^ kv_swz<D>(j * LR + r)) << 4));
-  }
+  row_offsets<D>(lane, voff);
   const int wv = uniform(wave);
-  const uint32_t lds0 = lds_addr(&buf[0][0]) + wv * 2 * NB * TB;
+  const uint32_t lds0 = uniform(int(lds_addr(&buf[0][0]) + wv * 2 * NB * TB));
 
   for (; !deal.done(); deal.next()) {
     const Tile& t = deal.t;
@@ -688,9 +709,8 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
     uint32_t at;   // where 16 rows at a time are, of the tile last asked for
     auto issue = [&](const char* base, uint32_t lds) {
 #pragma unroll
-      for (int j = 0; j < NI; ++j)
-        lds_load16s(base + int64_t(read_lane(at, j / NO)) * (D * 2) + (j % NO) * 1024, voff[j % NO],
-                    lds + j * 1024);
+      for (int j = 0; j < 2; ++j)
+        load_rows16(base + uint64_t(read_lane(at, j)) * (D * 2), voff, lds + j * NO * 1024);
     };
     auto issue_k = [&](int x) {
       const int key0 = key_of(x);
@@ -880,7 +900,6 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
   constexpr int KS = D / 16, DB = D / 32;
   constexpr int TB = BK * D * 2;             // bytes of a tile
   constexpr int NL = TB / 4096;              // loads of a thread per tile
-  constexpr int LR = 512 / D;                // rows of a wave's load
   constexpr int H = 8 * KB;                  // half the elements of a tile in a lane
   __shared__ __align__(1024) char sKb[2][TB];
   __shared__ __align__(1024) char sVb[2][TB];
@@ -890,13 +909,13 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
   const int c = lane & 31, g = lane >> 5;
   Deal<R, BLOCK, true> deal(a, sh, run_of_block(a.groups));
   const int ps = 1 << a.psl;
-  // A load's LR rows lie in one page (pages hold multiples of 16 rows), and
-  // their chunks' permutation does not depend on which load of the tile it is:
-  // one offset per lane serves all, the rest of the address is scalar.
-  const int wv = uniform(wave), lrow = lane / (D / 8);
-  const uint32_t voff = uint32_t(lrow * D * 2 + ((lane % (D / 8) ^ kv_swz<D>(wv * LR + lrow)) << 4));
-  const uint32_t ldsK = uniform(int(lds_addr(&sKb[0][0]) + wv * 1024));
-  const uint32_t ldsV = uniform(int(lds_addr(&sVb[0][0]) + wv * 1024));
+  // A wave loads 16 rows of a tile, which lie in one page (its rows are a multiple
+  // of 16): one look-up, one scalar address.
+  uint32_t voff[NL];
+  row_offsets<D>(lane, voff);
+  const int wv = uniform(wave);
+  const uint32_t ldsK = uniform(int(lds_addr(&sKb[0][0]) + wv * NL * 1024));
+  const uint32_t ldsV = uniform(int(lds_addr(&sVb[0][0]) + wv * NL * 1024));
 
   for (; !deal.done(); deal.next()) {
     const Tile& t = deal.t;
@@ -944,15 +963,13 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
       for (int ks = 0; ks < KS; ++ks) qf[ks] = as_bf16x8(ld16(qp + ks * 16));
     }
     wait_loads<KS>();   // the page ids have landed, Q may be on its way
-    // The first rows of this wave's loads of tile x.  (What rows past the last
-    // key hold is masked.)
-    auto locate = [&](int x) {   // lane j: load j
-      return pages.row_of(key_base + x * BK + ((lane & (NL - 1)) * 4 + wv) * LR, last, page_rows);
+    // The first of this wave's rows of tile x.  (What rows past the last key hold
+    // is masked.)
+    auto locate = [&](int x) {
+      return read_lane(pages.row_of(key_base + x * BK + wv * 16, last, page_rows), 0);
     };
     auto issue = [&](const char* base, uint32_t at, uint32_t lds) {
-#pragma unroll
-      for (int j = 0; j < NL; ++j)
-        lds_load16u(base + uint64_t(read_lane(at, j)) * (D * 2), voff, lds + j * 4096);
+      load_rows16(base + uint64_t(at) * (D * 2), voff, lds);
     };
     uint32_t at_v, at_k;   // of the V tile and of the K tile to be asked for next
     auto kfrag = [&](int buf, int j) {
