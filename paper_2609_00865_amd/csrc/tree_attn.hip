@@ -636,7 +636,7 @@ struct Pair {
 // of waits: dealt 8.4 us (about 0.5 for the lengths, 0.7 for the deal and 0.7 for
 // finding the run in it, 1.0 for page ids, 0.9 for the first keys, 1.1 for a tile
 // and 0.9 for the waves' joint result, the launch the rest) and 3.4 for the join;
-// whole 11.6, of one launch.
+// whole 11.1, of one launch.
 // Two waves to a workgroup and two workgroups to a CU (us: 101 and 413; four
 // waves and one workgroup 102 and 413, short runs 0 to 8 % slower; one wave and
 // four workgroups 128 and 488).  64 or 128 pairs to a wave were no faster.
@@ -888,8 +888,8 @@ __global__ __launch_bounds__(NW * 64) void tree_few_kernel(TreeArgs a) {
 // Where contexts are read once (24 trees of 8 to 61 tokens over 301 to 8192
 // rows, 28/4 heads of 128: 181 MB of keys and Q, 30 MB of partial results, 42
 // us, 5.0 TB/s) it is bound by memory; where rows are many (two chunks of 1531
-// to 2048 rows over 4099 to 8192, 420 GFLOP: 410 to 470 us with the chip's clock,
-// 0.9 to 1.0 PFLOP/s) by the matrix pipe, 58 % busy, and the six vector
+// to 2048 rows over 4099 to 8192, 420 GFLOP: 394 to 450 us with the chip's clock,
+// 0.93 to 1.06 PFLOP/s) by the matrix pipe, 58 % busy, and the six vector
 // instructions beside each MFMA that share its SIMD.  32-key tiles in four
 // buffers were 4 % slower on the chunks and 7 % at head_dim 64, up to 10 %
 // faster where runs are a few units; eight waves on 256 pairs were slower.
