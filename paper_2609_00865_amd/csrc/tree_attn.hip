@@ -1044,7 +1044,8 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
     auto odd_values = [&](const f32x16 (&s)[KB], int x, char* sV) __attribute__((always_inline)) {
       bool odd = false;
 #pragma unroll
-      for (int j = 0; j < NL; ++j) odd |= odd16(sV + (j * 4 + wv) * 1024 + (here(threadIdx.x) & 63) * 16);
+      for (int j = 0; j < NL; ++j)
+        odd |= odd16(sV + (j * 4 + wv) * 1024 + (here(threadIdx.x) & 63) * 16);
       if (!__syncthreads_or(odd)) return;
       const float mu = m_off();
       const uint32_t see0 = seen(x, 0), see1 = seen(x, 1);
@@ -1509,8 +1510,8 @@ hipError_t launch_tree_attn(const mv_cache_shape& cs, const CacheDev& cd, int la
 hipError_t launch_tree_mask(int B, int N, const int32_t* ptr, const int32_t* parent, int words,
                             uint32_t* tree, int32_t* depth, hipStream_t stream) {
   ProfScope prof("tree_mask", stream);
-  hipLaunchKernelGGL(tree_mask_kernel, dim3(unsigned((int64_t(N) + 255) / 256)), dim3(256), 0, stream, B, N, ptr,
-                     parent, words, tree, depth);
+  hipLaunchKernelGGL(tree_mask_kernel, dim3(unsigned((int64_t(N) + 255) / 256)), dim3(256), 0,
+                     stream, B, N, ptr, parent, words, tree, depth);
   return hipGetLastError();
 }
 
