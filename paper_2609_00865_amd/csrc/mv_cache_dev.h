@@ -43,7 +43,8 @@ __device__ __forceinline__ void lds_barrier() {
 
 // Inclusive prefix sum over the wave by data-parallel moves between lanes (six
 // vector instructions; through LDS the same six steps take ten times as long).
-__device__ __forceinline__ int wave_scan(int x) {
+// (Sums without a sign hold what passes 2^31.)
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
   constexpr int kShr = 0x110, kBcast15 = 0x142, kBcast31 = 0x143;
   x += __builtin_amdgcn_update_dpp(0, x, kShr + 1, 0xf, 0xf, false);
   x += __builtin_amdgcn_update_dpp(0, x, kShr + 2, 0xf, 0xf, false);

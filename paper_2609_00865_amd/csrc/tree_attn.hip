@@ -23,6 +23,7 @@
 #include <type_traits>
 
 #include "mv_cache_dev.h"
+#include "tree_deal.h"
 
 namespace mv {
 
@@ -64,7 +65,6 @@ struct TreeJoin {
   int pad[2];
 };
 
-constexpr int kUnit = 64;       // keys of a unit of work
 constexpr int kPlanB = 512;     // entries whose sizes are held in LDS
 constexpr int kChunks = 256;    // blocks of tile places whose first unit is held in LDS
 
@@ -76,14 +76,15 @@ struct Tile {
   int kmax;         // keys [0, kmax)
   // a tile without keys is one unit: its rows are still written
   __device__ __forceinline__ int units() const {
-    return rows ? max(1, (kmax + kUnit - 1) / kUnit) : 0;
+    return rows ? max(1, units_of(kmax)) : 0;
   }
 };
 
 struct TreeShared {
   int ptr[kPlanB + 1];
   int id[kPlanB], len[kPlanB];
-  int tmp[2][4];
+  uint32_t unit_tmp[4];         // of each wave's tiles
+  int tile_tmp[4];
   int64_t units[kChunks], tiles[kChunks];   // before each BLOCK of places
   Tile tile;                    // where a run begins
   int at;
@@ -212,35 +213,35 @@ struct Deal {
   }
 
   // The tiles of places [j BLOCK, (j + 1) BLOCK): units and tiles before each
-  __device__ __forceinline__ void scan(int j, Tile& mine, int (&before)[2], int (&sum)[2]) {
+  struct Before {
+    int64_t units;
+    int tiles;
+  };
+  __device__ __forceinline__ void scan(int j, Tile& mine, Before& before, Before& sum) {
     const TreeArgs& a = direct;
     const int u = j * BLOCK + threadIdx.x;
     mine = Tile{};
     if (u < a.tiles) mine = tile_of<R>(a, s, u);
     if (blockIdx.x == 0 && u < a.tiles && mine.rows == 0)   // no run comes by here
       for (int h = 0; h < a.Hkv; ++h) a.join[int64_t(u) * a.Hkv + h].rows = 0;
-    // (a tile has fewer than 2^25 units: BLOCK of them do not pass 2^31 unless
-    // the caches are past any memory, in which case the rows are unspecified)
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int units = mine.units(), x = wave_scan(units);
+    const uint32_t units = mine.units(), x = wave_scan(units);
     const uint64_t is = __ballot(mine.rows > 0);
-    lds_barrier();   // tmp of an earlier block of places is read
+    lds_barrier();   // what an earlier block of places left is read
     if (lane == 63) {
-      s.tmp[0][wave] = x;
-      s.tmp[1][wave] = __popcll(is);
+      s.unit_tmp[wave] = x;
+      s.tile_tmp[wave] = __popcll(is);
     }
     lds_barrier();
-    before[0] = x - units;
-    before[1] = __popcll(is & ((uint64_t(1) << lane) - 1));
-    sum[0] = sum[1] = 0;
+    add_waves<BLOCK / 64>(s.unit_tmp, wave, before.units, sum.units);
+    before.units += x - units;
+    before.tiles = __popcll(is & ((uint64_t(1) << lane) - 1));
+    sum.tiles = 0;
 #pragma unroll
     for (int w = 0; w < BLOCK / 64; ++w) {
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int n = s.tmp[e][w];
-        before[e] += w < wave ? n : 0;
-        sum[e] += n;
-      }
+      const int n = s.tile_tmp[w];
+      before.tiles += w < wave ? n : 0;
+      sum.tiles += n;
     }
   }
 
@@ -259,7 +260,7 @@ struct Deal {
     __syncthreads();
     const int chunks = (a.tiles + BLOCK - 1) / BLOCK;
     Tile mine;
-    int before[2] = {0, 0}, sum[2];
+    Before before{}, sum;
     int64_t units = 0, tiles = 0;
     for (int j = 0; j < chunks; ++j) {
       scan(j, mine, before, sum);
@@ -267,8 +268,8 @@ struct Deal {
         s.units[j] = units;
         s.tiles[j] = tiles;
       }
-      units += sum[0];
-      tiles += sum[1];
+      units += sum.units;
+      tiles += sum.tiles;
     }
     units = uniform(units);
     tiles = uniform(tiles);
@@ -293,7 +294,7 @@ struct Deal {
       x -= s.units[lo] + extra * s.tiles[lo];
       scan(lo, mine, before, sum);
     }
-    const int first = before[0] + extra * before[1];
+    const int64_t first = before.units + extra * before.tiles;
     if (mine.rows > 0 && x >= first && x < first + mine.units() + extra) {
       s.tile = mine;
       s.at = int(x) - first;

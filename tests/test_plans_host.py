@@ -89,3 +89,9 @@ def test_lm_head_backward_reserves_what_it_uses():
     assert _lm_sizes(32768, 3584, 152064)[2] <= both + 4096
     # three fp32 partials of the 1384 leaves' dh, beside G
     assert _lm_sizes(1384, 3584, 152064)[4] <= 2 * vp * 1536 + 3 * 4 * 1384 * 3584 + 65536
+
+
+def test_attention_units_past_31_bits(tmp_path):
+    """Tiles that see the same long sequence have more units together than 31
+    bits hold: their sums are those in 64 bits."""
+    _run(tmp_path, "tree_deal_check")
