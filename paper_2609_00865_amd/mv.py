@@ -800,8 +800,11 @@ def _token_stride(t, what):
 
 
 def _use(stream, *ts):
-    """The stream's handle; tensors made here on the current stream are kept
-    from reuse until `stream` is done with them."""
+    """The handle of the stream a call is queued on.  A given one waits for the
+    current stream first, in every call of the cache, its attention and the
+    rotary axes, so what was queued there (the call's inputs, the cache's state)
+    is seen; tensors made here on the current stream are kept from reuse until
+    `stream` is done with them."""
     if stream is None:
         return _stream()
     cur = torch.cuda.current_stream()
@@ -855,7 +858,7 @@ def rope_axes(x, pos, rope: RopeAxes, inverse: bool = False, out=None, stream=No
         handle, out_stride = _use(stream, out), heads * d
     else:
         _need(out, torch.bfloat16, "out", shape, contiguous=False)
-        handle, out_stride = _stream(stream), _token_stride(out, "out")
+        handle, out_stride = _use(stream), _token_stride(out, "out")
     check(mv_rope_axes(rope._ref, n, heads, d, x.data_ptr(), _token_stride(x, "x"),
                        pos.data_ptr(), -1 if inverse else 1, out.data_ptr(), out_stride, handle))
     return out
@@ -869,7 +872,9 @@ class PagedCache:
     device tensors: k, v bf16 [n_layers, n_pages, n_heads_kv, page_size,
     head_dim], page_table int32 [n_seqs, max_pages] (-1: none), seq_len int32
     [n_seqs], page_refs int32 [n_pages] (holders; 0: free).  New caches are
-    empty (the pools' contents are not set)."""
+    empty (the pools' contents are not set).  ``stream`` here and in the calls
+    on the cache: the stream to queue on, which waits for the current one first;
+    the current one does not wait for it."""
 
     def __init__(self, n_layers: int, n_pages: int, page_size: int, n_heads_kv: int,
                  head_dim: int, n_seqs: int, max_pages: int, device="cuda", stream=None):
@@ -922,7 +927,7 @@ class PagedCache:
         """free_pages, and the entries refused (for lack of pages, as malformed)
         since the last call; waits for the stream."""
         out = CacheCounts()
-        check(mv_cache_status(*self._args(), ctypes.byref(out), _stream(stream)))
+        check(mv_cache_status(*self._args(), ctypes.byref(out), _use(stream)))
         return out.as_dict()
 
 
@@ -969,7 +974,7 @@ def cache_write(cache: PagedCache, layer: int, slot, k, v, rope: Optional[RopeAx
     check(mv_cache_write(*cache._args(), int(layer), n, _ptr(slot), _ptr(k),
                          _token_stride(k, "k"), _ptr(v), _token_stride(v, "v"),
                          rope._ref if rope is not None else None,
-                         _ptr(pos) if rope is not None else None, _stream(stream)))
+                         _ptr(pos) if rope is not None else None, _use(stream)))
 
 
 def cache_workspace(cache: PagedCache, n: int) -> torch.Tensor:
@@ -1009,7 +1014,7 @@ def cache_compact(cache: PagedCache, src, dst, span_ptr, spans, workspace=None,
 def cache_free(cache: PagedCache, seq_ids, stream=None) -> None:
     """Empty the sequences and give their pages back."""
     _need_ids(seq_ids, "seq_ids")
-    check(mv_cache_free(*cache._args(), seq_ids.numel(), _ptr(seq_ids), _stream(stream)))
+    check(mv_cache_free(*cache._args(), seq_ids.numel(), _ptr(seq_ids), _use(stream)))
 
 
 # ---------------------------------------------------------------------------
