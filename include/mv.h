@@ -636,8 +636,12 @@ mv_status mv_rope_axes(const mv_rope_axes_spec* spec, int32_t n_tokens, int32_t 
  *               past a sequence's pages are -1
  *   seq_len     int32 [n_seqs]
  *   page_refs   int32 [n_pages]: sequences that hold the page; 0: free
- *   ctl         int32 [4]: the lowest page that may be free, refused entries
- *               for lack of pages, refused malformed entries, one word unused
+ *   ctl         int32 [4]: where the search for free pages begins (no page
+ *               below is free: the calls see to it), refused entries for lack
+ *               of pages, refused malformed entries, the free pages as the last
+ *               mv_cache_status counted them.  Whoever writes page_refs
+ *               themselves sets ctl[0] to 0 after: a free page below it would
+ *               not be found, though mv_cache_status counts it
  * The state lives on the device: every call is asynchronous, reads nothing
  * back, allocates nothing and may be captured into a graph.  It takes
  * lists of entries; entries are independent of each other and all read the

@@ -895,8 +895,9 @@ class PagedCache:
         self._refs = (ctypes.byref(self.shape), ctypes.byref(self.c))
         self.reset(stream)
 
-    # (the library holds their addresses: their contents may be set, they
-    # themselves not)
+    # (the library holds their addresses: the contents of k and v may be set,
+    # the tensors themselves not.  Tables, lengths and holders are set together,
+    # by restore(), which has the search for free pages begin at the first again.)
     k = property(lambda self: self._t[0])
     v = property(lambda self: self._t[1])
     page_table = property(lambda self: self._t[2])
@@ -914,7 +915,8 @@ class PagedCache:
         check(mv_cache_reset(*self._args(), _use(stream, *self._t)))
 
     def restore(self, page_table, seq_len, page_refs) -> None:
-        """Take over a state saved from (or laid out for) a cache of this shape."""
+        """Take over a state saved from (or laid out for) a cache of this shape,
+        on the current stream; refusals counted so far are forgotten."""
         for mine, theirs, what in ((self.page_table, page_table, "page_table"),
                                    (self.seq_len, seq_len, "seq_len"),
                                    (self.page_refs, page_refs, "page_refs")):
