@@ -807,6 +807,9 @@ def _use(stream, *ts):
     `stream` is done with them."""
     if stream is None:
         return _stream()
+    if stream.device.index != _device():
+        raise ValueError(f"the stream is of {stream.device}, the current device is "
+                         f"cuda:{_device()}")
     cur = torch.cuda.current_stream()
     if stream != cur:
         # what this call allocated may be a block whose last use is queued there

@@ -85,6 +85,17 @@ def test_on_the_current_stream_nothing_waits(calls):
         assert not cur.waited and handles[-2:] == [11, 11], name
 
 
+def test_a_stream_of_another_device_is_refused(calls):
+    """Kernels would run there, on pointers of the current device."""
+    todo, handles, cur = calls
+    for name, call in todo.items():
+        side = Stream(22)
+        side.device = torch.device("cuda", 1)
+        with pytest.raises(ValueError, match="stream"):
+            call(side)
+        assert not side.waited and not handles, name
+
+
 @pytest.mark.gpu
 def test_a_side_stream_sees_what_was_queued():
     """Rows that are still being computed on the current stream, written and
