@@ -227,6 +227,8 @@ mv_status mv_cache_reserve(const mv_cache_shape* s, const mv_cache* c, int32_t n
     if (mv_status st = check_words({seq_ids, new_ptr}); st != MV_OK) return st;
   if (n_new > 0)
     if (mv_status st = check_words({slot}); st != MV_OK) return st;
+  if (pos != nullptr)
+    if (mv_status st = check_words({pos}); st != MV_OK) return st;
   return hip_status(mv::launch_cache_reserve(d, n, seq_ids, new_ptr, n_new, slot, pos, stream),
                     "cache reserve launch");
 }
@@ -343,6 +345,8 @@ mv_status mv_tree_mask(int32_t n_batch, int32_t n_rows, const int32_t* row_ptr,
     return fail(MV_ERR_SHAPE, "n_rows >= 0 and 0 < words <= 2^20 required");
   if (n_batch == 0 || n_rows == 0) return MV_OK;
   if (mv_status st = check_words({row_ptr, parent, tree}); st != MV_OK) return st;
+  if (depth != nullptr)
+    if (mv_status st = check_words({depth}); st != MV_OK) return st;
   return hip_status(mv::launch_tree_mask(n_batch, n_rows, row_ptr, parent, words, tree, depth,
                                          stream),
                     "tree mask launch");
