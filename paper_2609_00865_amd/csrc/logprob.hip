@@ -277,11 +277,10 @@ __global__ __launch_bounds__(NWAVES * 64, 1) void lm_tile_kernel(LmArgs a) {
   constexpr bool PANELS = DH;
   constexpr bool GATHER = MODE == kModeKL || MODE == kModeKLGrad;
   constexpr uint32_t SSTEP = (PANELS ? PANEL : BKK) * 2;   // bytes from a row's k slice to the next
-  auto row_a = [&](int h, int q) {
-    return TA == 256 ? q * 128 + h * 64 + wave * 8
-                     : (wave >> 2) * 64 + h * 32 + (wave & 3) * 8;
-  };
-  auto row_b = [&](int h, int q) { return q * 128 + (wave >> 2) * 64 + h * 32 + (wave & 3) * 8; };
+  // a region's row: the wave's, and a constant
+  const int wave_b = (wave >> 2) * 64 + (wave & 3) * 8, wave_a = TA == 256 ? wave * 8 : wave_b;
+  auto row_a = [](int h, int q) { return TA == 256 ? q * 128 + h * 64 : h * 32; };
+  auto row_b = [](int h, int q) { return q * 128 + h * 32; };
   const size_t tile_a = TRA ? size_t(0) : PANELS ? panel_index(a0, kbeg * BKK, K) : size_t(a0) * K;
   const size_t tile_b = PANELS ? panel_index(t0, kbeg * BKK, K) : size_t(t0) * K;
   const char* baseA = reinterpret_cast<const char*>(uniform_ptr(A + tile_a));
@@ -295,8 +294,8 @@ __global__ __launch_bounds__(NWAVES * 64, 1) void lm_tile_kernel(LmArgs a) {
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
       const uint32_t ch = ((lane & 7) ^ (lane >> 3)) * 16;
-      const int ra = min(row_a(h, q) + (lane >> 3), a_rows - 1 - a0);
-      const int rb = min(row_b(h, q) + (lane >> 3), a.T - 1 - t0);
+      const int ra = min(wave_a + row_a(h, q) + (lane >> 3), a_rows - 1 - a0);
+      const int rb = min(wave_b + row_b(h, q) + (lane >> 3), a.T - 1 - t0);
       offA[h][q] = uint32_t(ra) * row_bytes + ch;
       offB[h][q] = uint32_t(rb) * row_bytes + ch;
       if (GATHER) {
@@ -323,22 +322,23 @@ __global__ __launch_bounds__(NWAVES * 64, 1) void lm_tile_kernel(LmArgs a) {
 #pragma unroll
       for (int q = 0; q < 2; ++q)
         lds_load16s(baseA + (size_t(k0) * a.H + min(a0 + (h + 2 * q) * 64, a.H - 64)) * 2, off,
-                    st + row_a(h, q) * 128);
+                    st + wave_a * 128, row_a(h, q) * 128);
       return;
     }
     const char* b = baseA + size_t(kk) * SSTEP;
 #pragma unroll
-    for (int q = 0; q < NQA; ++q) lds_load16s(b, offA[h][q], st + row_a(h, q) * 128);
+    for (int q = 0; q < NQA; ++q)
+      lds_load16s(b, offA[h][q], st + wave_a * 128, row_a(h, q) * 128);
   };
   auto issue_b = [&](int h, int kk) {
     const uint32_t st = lds0 + 2 * SLICE_B + (kk & 1) * SLICE_B;
     if (GATHER) {
-      lds_load16(rowB[h][0] + size_t(kk) * BKK, st + row_b(h, 0) * 128);
-      lds_load16(rowB[h][1] + size_t(kk) * BKK, st + row_b(h, 1) * 128);
+      lds_load16(rowB[h][0] + size_t(kk) * BKK, st + wave_b * 128, row_b(h, 0) * 128);
+      lds_load16(rowB[h][1] + size_t(kk) * BKK, st + wave_b * 128, row_b(h, 1) * 128);
     } else {
       const char* b = baseB + size_t(kk) * SSTEP;
-      lds_load16s(b, offB[h][0], st + row_b(h, 0) * 128);
-      lds_load16s(b, offB[h][1], st + row_b(h, 1) * 128);
+      lds_load16s(b, offB[h][0], st + wave_b * 128, row_b(h, 0) * 128);
+      lds_load16s(b, offB[h][1], st + wave_b * 128, row_b(h, 1) * 128);
     }
   };
 
@@ -607,8 +607,8 @@ __global__ __launch_bounds__(NWAVES * 64, 1) void lm_dw_kernel(LmArgs a) {
   auto issue_a = [&](int h, int kk) {
     const char* b = Gb + size_t(kk >> 2) * gstep + (kk & 3) * SUB;
     const uint32_t st = lds0 + (kk & 1) * SLICE_B + wave * 1024;
-    lds_load16s(b + size_t(h) * (PANEL * 2), goff, st + h * SUB);
-    lds_load16s(b + size_t(h + 2) * (PANEL * 2), goff, st + (h + 2) * SUB);
+    lds_load16s(b + size_t(h) * (PANEL * 2), goff, st, h * SUB);
+    lds_load16s(b + size_t(h + 2) * (PANEL * 2), goff, st, (h + 2) * SUB);
   };
   auto issue_b = [&](int h, int kk) {
     const int k0 = kk * BKK;   // < T
@@ -617,8 +617,8 @@ __global__ __launch_bounds__(NWAVES * 64, 1) void lm_dw_kernel(LmArgs a) {
     // hidden columns past H (whole sub-tiles) read the last ones: outputs skipped
 #pragma unroll
     for (int q = 0; q < 2; ++q)
-      lds_load16s(Hb + size_t(k0) * hrow_bytes + min(t0 + (2 * h + q) * 64, a.H - 64) * 2, off,
-                  st + (2 * h + q) * SUB);
+      lds_load16s(Hb + size_t(k0) * hrow_bytes + min(t0 + (2 * h + q) * 64, a.H - 64) * 2, off, st,
+                  (2 * h + q) * SUB);
   };
 
   // Transposing operand read in natural k order (rows g*8 + 0..7 of a k step

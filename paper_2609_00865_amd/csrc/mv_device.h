@@ -37,32 +37,39 @@ __device__ __forceinline__ bf16x8 as_bf16x8(uint4 v) { return __builtin_bit_cast
 // may also use (and does not let inline asm clobber), so each helper saves it
 // in a scratch SGPR and restores it right after the issue: from the
 // compiler's view M0 is unchanged.  (The hardware reads M0 when the load is
-// issued.)  The compiler's own LDS-DMA builtins are not used because it
+// issued, and M0 has to be written a wait state earlier: hence the s_nop,
+// which the compiler adds for its own loads but not inside an asm statement.
+// The add that forms the address writes M0 itself, which pays for the state:
+// the LM head of 32768 tokens x 3584 x 152064 takes 23.5 ms forward, 49.1
+// backward and 29.4 for dW, with neither 25.0, 50.7 and 28.7; a move and the
+// state made dH 6 % slower.)  The compiler's own LDS-DMA builtins are not used because it
 // cannot tell which LDS buffer they write and would wait for every load in
 // flight before any LDS read.
 // 16 bytes per lane from global memory straight into LDS: lane l's data lands
-// at LDS byte address lds + 16 l (lds is the wave's base, uniform across the
-// wave).  The load is counted by vmcnt only; the compiler does not track it,
-// so the caller waits with wait_vmcnt before a barrier that publishes it.
-__device__ __forceinline__ void lds_load16(const void* src, uint32_t lds) {
+// at LDS byte address lds + add + 16 l (lds is the wave's base, uniform across
+// the wave; add is a constant).  The load is counted by vmcnt only; the compiler
+// does not track it, so the caller waits with wait_vmcnt before a barrier that
+// publishes it.
+__device__ __forceinline__ void lds_load16(const void* src, uint32_t lds, uint32_t add) {
   uint32_t saved;
   asm volatile(
-      "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %1, off\n\t"
-      "s_mov_b32 m0, %0"
+      "s_mov_b32 %0, m0\n\ts_add_u32 m0, %2, %3\n\ts_nop 0\n\t"
+      "global_load_lds_dwordx4 %1, off\n\ts_mov_b32 m0, %0"
       : "=&s"(saved)
-      : "v"(src), "s"(__builtin_amdgcn_readfirstlane(lds))
-      : "memory");
+      : "v"(src), "s"(__builtin_amdgcn_readfirstlane(lds)), "i"(add)
+      : "memory", "scc");
 }
 
 // The same with a wave-uniform base address and a byte offset per lane.
-__device__ __forceinline__ void lds_load16s(const void* base, uint32_t off, uint32_t lds) {
+__device__ __forceinline__ void lds_load16s(const void* base, uint32_t off, uint32_t lds,
+                                            uint32_t add) {
   uint32_t saved;
   asm volatile(
-      "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\tglobal_load_lds_dwordx4 %1, %2\n\t"
-      "s_mov_b32 m0, %0"
+      "s_mov_b32 %0, m0\n\ts_add_u32 m0, %3, %4\n\ts_nop 0\n\t"
+      "global_load_lds_dwordx4 %1, %2\n\ts_mov_b32 m0, %0"
       : "=&s"(saved)
-      : "v"(off), "s"(base), "s"(__builtin_amdgcn_readfirstlane(lds))
-      : "memory");
+      : "v"(off), "s"(base), "s"(__builtin_amdgcn_readfirstlane(lds)), "i"(add)
+      : "memory", "scc");
 }
 
 // A wave-uniform pointer taken through readfirstlane, so that it is held in
@@ -108,25 +115,25 @@ __device__ __forceinline__ rsrc_t make_rsrc(const void* base, uint32_t bytes) {
                                            __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
 }
 // 16 bytes per lane from a raw buffer straight into LDS: lane l's data
-// lands at LDS byte address lds + 16 l (lds uniform across the wave).  As
+// lands at LDS byte address lds + add + 16 l (lds uniform across the wave).  As
 // with lds_load16 the load is counted by vmcnt only; the caller waits with
 // wait_vmcnt before the barrier that publishes it.  Offsets must stay in
 // range (an out-of-range lane's LDS bytes are not relied upon).
-__device__ __forceinline__ void buf_lds16(rsrc_t r, uint32_t off, uint32_t lds) {
+__device__ __forceinline__ void buf_lds16(rsrc_t r, uint32_t off, uint32_t lds, uint32_t add) {
   uint32_t saved;
   asm volatile(
-      "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds\n\t"
-      "s_mov_b32 m0, %0"
+      "s_mov_b32 %0, m0\n\ts_add_u32 m0, %3, %4\n\ts_nop 0\n\t"
+      "buffer_load_dwordx4 %1, %2, 0 offen lds\n\ts_mov_b32 m0, %0"
       : "=&s"(saved)
-      : "v"(off), "s"(r), "s"(__builtin_amdgcn_readfirstlane(lds))
-      : "memory");
+      : "v"(off), "s"(r), "s"(__builtin_amdgcn_readfirstlane(lds)), "i"(add)
+      : "memory", "scc");
 }
 // 4 bytes per lane from a raw buffer straight into LDS (lane l at lds + 4 l).
 __device__ __forceinline__ void buf_lds4(rsrc_t r, uint32_t off, uint32_t lds) {
   uint32_t saved;
   asm volatile(
-      "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\tbuffer_load_dword %1, %2, 0 offen lds\n\t"
-      "s_mov_b32 m0, %0"
+      "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\t"
+      "buffer_load_dword %1, %2, 0 offen lds\n\ts_mov_b32 m0, %0"
       : "=&s"(saved)
       : "v"(off), "s"(r), "s"(__builtin_amdgcn_readfirstlane(lds))
       : "memory");
@@ -249,7 +256,7 @@ struct KvTileLoader {
 #pragma unroll
     for (int r = 0; r < KLD; ++r) {
       const uint32_t off = uint32_t(min(kt * BK + row[r], T - 1)) * kv_row + col[r];
-      buf_lds16(rs, off, lds + wv + r * 4096);
+      buf_lds16(rs, off, lds + wv, r * 4096);
     }
   }
   // K and V of key tile kt into the tiles at LDS byte addresses ldsK, ldsV
@@ -258,8 +265,8 @@ struct KvTileLoader {
 #pragma unroll
     for (int r = 0; r < KLD; ++r) {
       const uint32_t off = uint32_t(min(kt * BK + row[r], T - 1)) * kv_row + col[r];
-      buf_lds16(krs, off, ldsK + wv + r * 4096);
-      buf_lds16(vrs, off, ldsV + wv + r * 4096);
+      buf_lds16(krs, off, ldsK + wv, r * 4096);
+      buf_lds16(vrs, off, ldsV + wv, r * 4096);
     }
   }
 };
