@@ -31,17 +31,17 @@
 // matrix pipe is not waiting behind LDS reads, and quarter by quarter the
 // slice's LDS regions are free for the slice after next (a load has 1.5
 // slices to land).  Bound by the matrix pipe at the clock the chip holds
-// under it: at 32768 tokens x 3584 x 152064, on two boxes, the pipe is busy
-// 81-82% (logits), 73-75% (G) and 93% (dH) of the cycles at 1.76-1.81,
-// 1.78-1.87 and 1.59-1.64 GHz, where the earlier loop (both waves reading, then
-// both in MFMAs; one barrier per slice) had 56-64%.  Both timed in turn: at 4001 tokens logits 3.54 -> 3.22 ms, G 3.73 ->
-// 3.20, dH 3.50 -> 3.11; at 32768: 26.7 -> 24.5, 28.6 -> 26.0, 26.0 -> 23.1.  An
-// operand slice sits in LDS as [256 rows][64] bf16 without padding, with
-// 16-byte chunk c of row r at chunk position c ^ (r & 7): the fragment reads
-// (16 lanes = 16 consecutive rows at one chunk) hit distinct banks.  Tiles are
-// ordered so that the blocks resident on one XCD at a time form a compact 2-D
-// patch (a few token tiles x several A tiles) and share operand slices in that
-// XCD's L2.
+// under it: at 32768 tokens x 3584 x 152064 the pipe is busy 87% (logits), 79%
+// (G) and 97% (dH) of the cycles at 1.68-1.73, 1.75 and 1.55 GHz, where the
+// earlier loop (both waves reading, then both in MFMAs; one barrier per slice)
+// had 56-64%.  Both timed in turn, before a load's LDS address went to M0 by the
+// add that forms it: at 4001 tokens logits 3.54 -> 3.22 ms, G 3.73 -> 3.20, dH
+// 3.50 -> 3.11; at 32768: 26.7 -> 24.5, 28.6 -> 26.0, 26.0 -> 23.1.  An operand
+// slice sits in LDS as [256 rows][64] bf16 without padding, with 16-byte chunk
+// c of row r at chunk position c ^ (r & 7): the fragment reads (16 lanes = 16
+// consecutive rows at one chunk) hit distinct banks.  Tiles are ordered so that
+// the blocks resident on one XCD at a time form a compact 2-D patch (a few token
+// tiles x several A tiles) and share operand slices in that XCD's L2.
 #include <algorithm>
 #include <type_traits>
 
@@ -580,8 +580,8 @@ __global__ __launch_bounds__(NWAVES * 64, 1) void lm_tile_kernel(LmArgs a) {
 // 256 (the grad pass writes them), so the last slice needs no masking: H rows
 // past T are read clamped and meet zero G rows.  Bound as the tile engine: at
 // 32768 tokens x 3584 x 152064 the loop in which both waves of a SIMD read and
-// multiplied together took 31.7 ms with the pipe 64% busy, this one 28.3 ms
-// with 85%.
+// multiplied together took 31.7 ms with the pipe 64% busy, this one 29.3 ms
+// with 83% (28.3 and 85% without the wait state of its loads).
 __global__ __launch_bounds__(NWAVES * 64, 1) void lm_dw_kernel(LmArgs a) {
   __shared__ __align__(1024) u16 smem[2 * 2 * SLICE_B / 2];   // (G, H) x 2 slices
   constexpr int SUB = 64 * 128;   // bytes of a sub-tile
