@@ -736,6 +736,7 @@ mv_status mv_cache_fork(const mv_cache_shape* shape, const mv_cache* cache, int3
  * stay (dst == src) or become shared; the kept rows from there on are copied
  * to new pages, and with dst == src the old ones are given back (rows cut off
  * at the end alone are just dropped, unless a part-filled last page is shared).
+ * A row that moves walks the entry's spans: neighbouring rows belong in one.
  * dst[e] must be src[e] or empty; no dst twice; a sequence compacted in place
  * is no other entry's source.
  */
@@ -759,8 +760,9 @@ mv_status mv_cache_free(const mv_cache_shape* shape, const mv_cache* cache, int3
  * `tree`: bit a % 32 of word a / 32 stands for new row a of the same entry (a
  * row past its words is not seen).
  *     o = softmax(scale * q.k) v,   lse = log sum exp(scale * q.k)
- * over the rows seen; a row that sees none (seq_ids -1 or out of range, a
- * sequence shorter than n) gets o = 0, lse = -inf.  What a row does not see
+ * over the rows seen; a row that sees none (seq_ids -1 or out of range, an
+ * empty context and no bit, a row before the first of a sequence shorter than
+ * n) gets o = 0, lse = -inf.  What a row does not see
  * has no influence on it, infinities and NaN included.
  * q, o bf16 [n_rows, n_heads_q, head_dim]; lse fp32 [n_heads_q, n_rows];
  * row_ptr int32 [n_batch + 1], row_ptr[0] = 0, non-decreasing, at most n_rows;

@@ -14,7 +14,12 @@
 // of 128: 620 MB in 110 to 127 us, at or above a large copy's 4.9 TB/s), the others are
 // chains of dependent reads and barriers: reserve 6.8 us (16 sequences), plan 6.2
 // (32 forks) and 5.1 (the edit above), release 4.8 (32 sequences) and 7.1 (one of
-// 2048 pages), move 5.2 (the part-filled pages of 32 forks).
+// 2048 pages), move 5.2 (the part-filled pages of 32 forks).  These are of pools
+// of a round or two of the search (4096 pages each): with the free pages behind
+// 65536 or 250000 held ones a reservation takes 19 or 53 us.  A wave fills the
+// slots of an entry, so a prompt's 32768 rows take 71 us, and a row that moves
+// walks its entry's spans, so many of one row each cost more than the bytes (the
+// edit above into a branch: 0.21 ms with 16, 4.3 ms with 4096).
 #include "mv_cache_dev.h"
 
 namespace mv {

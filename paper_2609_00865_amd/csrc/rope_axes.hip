@@ -4,7 +4,8 @@
 // by its heads, so a block takes them once into LDS, and reads its first
 // elements meanwhile.  32768 tokens of 32 heads of 128: 100 us, 537 MB, 5.4 TB/s;
 // 64 tokens 3.4 us, a write of 16 sequences' 6 to 24 rows 3.9 us (an empty
-// launch: 2.1).
+// launch: 2.1), of a prompt's 32768 rows of 4 heads of 128 22 us as they are (134
+// MB, 6 TB/s) and 42 rotated (a token to a block: its angles are waited for).
 #include "mv_cache_dev.h"
 
 namespace mv {

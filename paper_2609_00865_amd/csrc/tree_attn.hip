@@ -65,7 +65,9 @@ struct TreeJoin {
   int pad[2];
 };
 
-constexpr int kPlanB = 512;     // entries whose sizes are held in LDS
+// Entries whose sizes are held in LDS; those of more are read from memory (single
+// tokens over 16 rows each: 512 of them 39 us, 513 50).
+constexpr int kPlanB = 512;
 constexpr int kChunks = 256;    // blocks of tile places whose first unit is held in LDS
 
 // One tile: the entry, its first pair, and the keys any of its rows may see.
@@ -1006,7 +1008,9 @@ __global__ __launch_bounds__(256, 2) void tree_many_kernel(TreeArgs a) {
     };
     // As in the masked forward: probabilities are taken against the maximum of
     // a tile that the row has scored before; only where they would pass 2^16,
-    // or a row has seen no key yet, is the tile's own maximum taken.
+    // or a row has seen no key yet, is the tile's own maximum taken.  They are
+    // rounded to bf16 for the product, as in the kernel for few pairs (outputs are
+    // then 2.3e-3 from 64 bits in norm, where their own rounding gives 1.7e-3).
     auto m_off = [&]() { return m_run == -INFINITY ? 0.f : m_run; };
     auto pexp = [&](const f32x16 (&s)[KB], int i, float mu) {
       return fast_exp2(fmaf(s[i >> 4][i & 15], a.scale_log2, -mu));
